@@ -259,6 +259,84 @@ int fps_attn_fwd(const fps_shape* shape, const fps_window* win, fps_precision pr
                  const float* sq, const float* sk, const float* sv, fps_vscale vscale, void* out,
                  fps_out_dtype out_dt, fps_layout out_layout, uint8_t* visited, void* stream);
 
+/* ---- before and after the attention ---------------------------------------------------------
+ * What a layer does around fps_attn_fwd: the products that make Q, K and V from the hidden states and take the output back
+ * (fps_mx4_*), and the norm and rotation of Q and K between the first product and the attention (fps_norm_rotate*). */
+
+/* A device tensor [B, heads, rows, cols] of type dt in the caller's own layout: element (b,h,r,c) lies at
+ * b*stride_b + h*stride_h + r*stride_r + c elements from data, which is 16-byte aligned like every device pointer; strides
+ * are not negative, and that of an axis of one element does not count.  Raster order is stride_r = cols, stride_h = rows*cols;
+ * a projection's rows [B, rows, heads*cols] are stride_h = cols, stride_r = the row's length, of which the heads may be a
+ * part (Q's third of the rows of one product for Q, K and V).  Inputs may repeat elements (stride 0); in an output no two
+ * elements may share a place, and it may share memory with an input only where the entry point says so. */
+typedef struct {
+    void* data;
+    fps_out_dtype dt;
+    int B, heads, rows, cols;
+    int64_t stride_b, stride_h, stride_r;
+} fps_view;
+
+/* Norm over the 128 channels of each token of each head: x -> x * (mean(x^2) + eps)^(-1/2) * weight, in fp32.
+ * weight: fp32 (device), [128] or, per_head != 0, [heads,128]; NULL = ones.  eps is a normal float > 0. */
+typedef struct { const float* weight; int per_head; float eps; } fps_norm;
+
+typedef enum {
+    FPS_PAIRS_ADJACENT = 0,   /* pair p is channels 2p and 2p + 1                                 */
+    FPS_PAIRS_HALVES = 1      /* pair p is channels p and p + 64                                  */
+} fps_pairing;
+
+/* Rotation by the token's place: pair p of token (t,h,w), (x,y) -> (x cos - y sin, x sin + y cos).  The first pairs_t pairs
+ * turn with t, the next pairs_h with h, the next pairs_w with w; what is left of the 64 stays.  table: fp32 (device), (cos, sin)
+ * of [T,pairs_t], then [H,pairs_h], then [W,pairs_w], not looked at if no pair turns; stride_b is the distance in floats between the tables of two batch
+ * elements, even and not negative, 0 if they share one.  It is as long as the axes, not as the tokens: 20 KB at 720p, which stay in the caches
+ * while the tokens pass. */
+typedef struct {
+    const float* table;
+    int64_t stride_b;
+    int pairs_t, pairs_h, pairs_w;
+    fps_pairing pairing;
+} fps_rotation;
+
+/* Floats of one batch element's table for shape's grid, or 0 on an invalid shape or rotation (table is not looked at). */
+size_t fps_rotation_floats(const fps_shape* shape, const fps_rotation* rot);
+
+/* Host: fills such a table (host memory): pair i of an axis of n pairs turns by place * base^(-i/n), where the first token of
+ * the axis has place start[axis].  Angles, cosines and sines are computed in 64 bits, so that far places keep their phase. */
+int fps_rotation_table_host(const fps_shape* shape, const fps_rotation* rot, const int64_t start[3], double base, float* table);
+
+/* Norm, then rotation, in one pass.  x and y: [B,heads,T*H*W,128], tokens in raster order, bf16 or fp32 each; rows are 16-byte
+ * aligned (strides are multiples of 8 elements in bf16, 4 in fp32).  norm or rot may be NULL: without that step.  Computed in
+ * fp32 and rounded once, at the end.  y may be x itself (the same data, type and strides).  Of shape the grid, B and heads
+ * count; its tile only has to be valid.  A row that holds an infinity or a NaN, or whose squares' sum passes fp32's
+ * range, gives such values itself and leaves the other rows alone. */
+int fps_norm_rotate(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
+                    const fps_view* y, void* stream);
+
+/* Norm, rotation and operand packing of Q or K (role; V has neither) in one pass: the operands that fps_attn_fwd takes, from x
+ * as in fps_norm_rotate.  FPS_PREC_FP8: as fps_quantize_raster, from the fp32 values of the rotation: scale = amax/448 of a
+ * scale group (1.0 for zeros), code = round-to-nearest-even of x/scale computed in fp32.  scales_out [B,heads,M*NS].
+ * FPS_PREC_BF16: as fps_pack_raster_bf16; scales_out is ignored and may be NULL.  A group that holds an infinity or a NaN has such a scale. */
+int fps_norm_rotate_operand(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
+                            fps_role role, fps_precision prec, void* xq_out, float* scales_out, void* stream);
+
+/* Bytes of workspace of fps_norm_rotate_bwd, or 0 on an invalid shape or norm. */
+size_t fps_norm_rotate_bwd_bytes(const fps_shape* shape, const fps_norm* norm);
+
+/* The gradient of fps_norm_rotate: from x and dy, the gradient of y, dx and, unless it is NULL, dweight (device, fp32,
+ * shaped like norm->weight; NULL where that is; summed over all tokens, batches and, if the heads share a weight, heads, in an order that only the
+ * shape determines).  x, dy and dx have one type; dx may be x or dy itself.  Quantisation by fps_norm_rotate_operand
+ * is passed straight through by the same call.  workspace: device memory of fps_norm_rotate_bwd_bytes(), free again when the
+ * call has run; FPS_ERR_WORKSPACE if it is smaller. */
+int fps_norm_rotate_bwd(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
+                        const fps_view* dy, const fps_view* dx, float* dweight, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* The values that packed E4M3 operands stand for, code * scale (Eq. 1's X^): packed codes of `role` and their scales (device,
+ * from fps_quantize_* or fps_norm_rotate_operand; per channel for V with FPS_VSCALE_CHANNEL) -> raster [B,heads,T,H,W,128] of
+ * type dt (device).  Inverse of the operand's layout; `vscale` is ignored for roles Q and K. */
+int fps_dequantize(const fps_shape* shape, const void* xq, const float* scales, fps_role role, fps_vscale vscale,
+                   fps_out_dtype dt, void* x_raster, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

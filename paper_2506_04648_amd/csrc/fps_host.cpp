@@ -119,7 +119,7 @@ static int check_window(const fps_window* w) {
     return FPS_OK;
 }
 
-static int check_enum(int v, int hi, const char* name) {
+int check_enum(int v, int hi, const char* name) {
     if (v < 0 || v > hi) { set_error("%s has invalid value %d", name, v); return FPS_ERR_INVALID_ARG; }
     return FPS_OK;
 }
@@ -127,8 +127,6 @@ static int check_enum(int v, int hi, const char* name) {
 }  // namespace fps
 
 using namespace fps;
-
-#define FPS_TRY(expr) do { int _rc = (expr); if (_rc != FPS_OK) return _rc; } while (0)
 
 extern "C" {
 

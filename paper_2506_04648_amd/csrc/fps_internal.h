@@ -170,9 +170,13 @@ __device__ __forceinline__ void load_arguments() {
     asm volatile("" ::"s"(x));
 }
 
+// where an entry point ends on the first argument that is refused
+#define FPS_TRY(expr) do { int _rc = (expr); if (_rc != FPS_OK) return _rc; } while (0)
+
 void set_error(const char* fmt, ...);
 int check_shape(const fps_shape* s, Geom* g);          // validates, fills g
 int check_ptr(const void* p, const char* name);        // non-null and 16-byte aligned
+int check_enum(int v, int hi, const char* name);
 int hip_fail(hipError_t e, const char* what);          // records and returns FPS_ERR_HIP
 
 // kernel launchers (defined in the .hip files); all arguments already validated
@@ -186,6 +190,16 @@ int launch_unpack_q8(const Geom& g, const void* xq, int role, uint8_t* out, hipS
 int launch_attn(const Geom& g, const fps_window& win, int prec, const void* q, const void* k,
                 const void* v, const float* sq, const float* sk, const float* sv, int vscale,
                 void* out, int out_f32, int out_raster, uint8_t* visited, hipStream_t st);
+
+int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, const fps_rotation* rot, const fps_view& y,
+                       hipStream_t st);
+int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm* norm, const fps_rotation* rot, int role,
+                               int prec, void* xq, float* scales, hipStream_t st);
+size_t norm_rotate_bwd_bytes(const Geom& g, int heads, bool per_head);
+int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* norm, const fps_rotation* rot, const fps_view& dy,
+                           const fps_view& dx, float* dweight, float* partial, hipStream_t st);
+int launch_dequantize(const Geom& g, const void* xq, const float* scales, int role, bool per_channel, bool f32, void* out,
+                      hipStream_t st);
 
 int launch_copy(const void* in, void* out, long long bytes, hipStream_t st);
 int launch_mfma_rate(int workgroups, int iters, float* sink, hipStream_t st);

@@ -21,6 +21,7 @@ PREC_BF16, PREC_FP8 = 0, 1
 VSCALE_TILE, VSCALE_CHANNEL = 0, 1
 ROLE_Q, ROLE_K, ROLE_V = 0, 1, 2
 OUT_BF16, OUT_F32 = 0, 1
+PAIRS_ADJACENT, PAIRS_HALVES = 0, 1
 LAYOUT_TILED, LAYOUT_RASTER = 0, 1
 EDGE_TRUNCATE, EDGE_SHIFT = 0, 1
 
@@ -30,7 +31,10 @@ EXPORTS = ("fps_last_error", "fps_schedule_select", "fps_num_tiles", "fps_num_gr
            "fps_quantize_raster",
            "fps_pack_tiles_bf16", "fps_pack_raster_bf16", "fps_debug_unpack_q8", "fps_debug_copy", "fps_debug_scores_q8",
            "fps_debug_scores_block_q8", "fps_debug_mfma_rate", "fps_debug_issue_mix",
-           "fps_attn_fwd")
+           "fps_attn_fwd", "fps_rotation_floats", "fps_rotation_table_host", "fps_norm_rotate", "fps_norm_rotate_operand",
+           "fps_norm_rotate_bwd_bytes", "fps_norm_rotate_bwd", "fps_dequantize")
+SIZES = ("fps_num_tiles", "fps_num_groups", "fps_tile_slots", "fps_block_slots", "fps_packed_bytes", "fps_rotation_floats",
+         "fps_norm_rotate_bwd_bytes")                      # exports that return a size, 0 for a refusal
 
 
 class Shape(ctypes.Structure):
@@ -50,6 +54,20 @@ class Regime(ctypes.Structure):
 class StepCfg(ctypes.Structure):
     _fields_ = [("step", ctypes.c_int), ("num_steps", ctypes.c_int), ("alpha1", ctypes.c_float),
                 ("alpha2", ctypes.c_float), ("regime", Regime * 3)]
+
+
+class View(ctypes.Structure):
+    _fields_ = ([("data", ctypes.c_void_p)] + [(n, ctypes.c_int) for n in ("dt", "B", "heads", "rows", "cols")]
+                + [(n, ctypes.c_int64) for n in ("stride_b", "stride_h", "stride_r")])
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("per_head", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = ([("table", ctypes.c_void_p), ("stride_b", ctypes.c_int64)]
+                + [(n, ctypes.c_int) for n in ("pairs_t", "pairs_h", "pairs_w", "pairing")])
 
 
 class FpsError(RuntimeError):
@@ -82,15 +100,10 @@ def lib():
         L.fps_last_error.restype = ctypes.c_char_p
         L.fps_last_error.argtypes = []
         L.fps_schedule_select.argtypes = [ctypes.POINTER(StepCfg), ctypes.POINTER(Regime)]
-        L.fps_num_tiles.restype = ctypes.c_size_t
         L.fps_num_tiles.argtypes = [ctypes.POINTER(Shape)]
-        L.fps_num_groups.restype = ctypes.c_size_t
         L.fps_num_groups.argtypes = [ctypes.POINTER(Shape)]
-        L.fps_tile_slots.restype = ctypes.c_size_t
         L.fps_tile_slots.argtypes = [ctypes.POINTER(Shape)]
-        L.fps_block_slots.restype = ctypes.c_size_t
         L.fps_block_slots.argtypes = [ctypes.POINTER(Shape)]
-        L.fps_packed_bytes.restype = ctypes.c_size_t
         L.fps_packed_bytes.argtypes = [ctypes.POINTER(Shape), ip]
         L.fps_tile_mask_host.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Window), vp,
                                          ctypes.POINTER(ctypes.c_uint64)]
@@ -109,10 +122,17 @@ def lib():
         L.fps_debug_issue_mix.argtypes = [ip, ip, ip, ip, ip, ip, vp, vp, vp]
         L.fps_attn_fwd.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Window), ip,
                                    ctypes.POINTER(StepCfg), vp, vp, vp, vp, vp, vp, ip, vp, ip, ip, vp, vp]
+        shape, view, norm, rot = (ctypes.POINTER(t) for t in (Shape, View, Norm, Rotation))
+        L.fps_rotation_floats.argtypes = [shape, rot]
+        L.fps_rotation_table_host.argtypes = [shape, rot, ctypes.POINTER(ctypes.c_int64), ctypes.c_double, vp]
+        L.fps_norm_rotate.argtypes = [shape, view, norm, rot, view, vp]
+        L.fps_norm_rotate_operand.argtypes = [shape, view, norm, rot, ip, ip, vp, vp, vp]
+        L.fps_norm_rotate_bwd_bytes.argtypes = [shape, norm]
+        L.fps_norm_rotate_bwd.argtypes = [shape, view, norm, rot, view, view, vp, vp, ctypes.c_size_t, vp]
+        L.fps_dequantize.argtypes = [shape, vp, vp, ip, ip, ip, vp, vp]
         for name in EXPORTS:
-            if name not in ("fps_last_error", "fps_num_tiles", "fps_num_groups", "fps_tile_slots",
-                            "fps_block_slots", "fps_packed_bytes"):
-                getattr(L, name).restype = ctypes.c_int
+            if name != "fps_last_error":
+                getattr(L, name).restype = ctypes.c_size_t if name in SIZES else ctypes.c_int
         _lib = L
     return _lib
 
@@ -345,4 +365,174 @@ def attn_fwd(shape: Shape, window, prec, q, k, v, sq=None, sk=None, sv=None, vsc
                               None if sv is None else sv.data_ptr(), vscale, out.data_ptr(), dt,
                               LAYOUT_RASTER if raster_out else LAYOUT_TILED,
                               None if visited is None else visited.data_ptr(), _stream()))
+    return out
+
+
+# ---- before and after the attention -------------------------------------------------------------
+def _here(*tensors):
+    """Every tensor (None: left out) is on the current device, whose stream the call goes to."""
+    torch = _torch or _import_torch()
+    device = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != device):
+            raise ValueError(f"a tensor on {t.device}, not on the current device (cuda:{device})")
+
+
+def _whole(t, dtype, numel, name):
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} of {numel} elements, not {t.dtype} {tuple(t.shape)}")
+
+
+def _dtype_code(t):
+    torch = _torch or _import_torch()
+    if t.dtype == torch.bfloat16:
+        return OUT_BF16
+    if t.dtype == torch.float32:
+        return OUT_F32
+    raise ValueError(f"{t.dtype} instead of bfloat16 or float32")
+
+
+def _view(t, name) -> View:
+    """[B, heads, tokens.., cols] of any strides; axes of tokens must follow each other in memory as in the shape."""
+    if t.dim() < 4:
+        raise ValueError(f"{name} must be [B, heads, tokens.., channels], not {tuple(t.shape)}")
+    size, stride = t.shape, t.stride()
+    rows, at = 1, 0
+    for n, s in zip(reversed(size[2:-1]), reversed(stride[2:-1])):
+        if n == 1:
+            continue
+        if rows == 1:
+            at = s
+        elif s != at * rows:
+            raise ValueError(f"{name}: the token axes of strides {stride[2:-1]} are not one axis")
+        rows *= n
+    if stride[-1] != 1 and size[-1] > 1:
+        raise ValueError(f"{name}: the channels must be contiguous")
+    return View(t.data_ptr(), _dtype_code(t), size[0], size[1], rows, size[-1], stride[0], stride[1], at)
+
+
+def make_norm(weight=None, eps=1e-6) -> Norm:
+    """Norm of each token of each head; weight: fp32 [128], or [heads, 128] for one of each head, or None."""
+    if weight is not None:
+        torch = _torch or _import_torch()
+        if weight.dtype != torch.float32 or weight.dim() not in (1, 2) or weight.shape[-1] != 128 or not weight.is_contiguous():
+            raise ValueError(f"a norm's weight is contiguous fp32 [128] or [heads, 128], not {weight.dtype} {tuple(weight.shape)}")
+    norm = Norm(_ptr(weight), weight is not None and weight.dim() == 2, eps)
+    norm.tensor = weight                                   # lives as long as the pointer to it
+    return norm
+
+
+def rotation_table(shape: Shape, split, base=10000.0, start=(0, 0, 0)):
+    """The rotation's table of shape's grid on the host, fp32 [entries, 2] from angles in 64 bits: `split` pairs turn with t, h
+    and w, pair i of n by place * base^(-i/n); start: place of the first frame, row and column."""
+    torch = _torch or _import_torch()
+    rot = Rotation(None, 0, *split, PAIRS_ADJACENT)
+    n = int(lib().fps_rotation_floats(ctypes.byref(shape), ctypes.byref(rot)))
+    if n == 0 and sum(split) != 0:
+        raise FpsError(FPS_ERR_INVALID_ARG, last_error())
+    table = torch.empty((n // 2, 2), dtype=torch.float32)
+    _check(lib().fps_rotation_table_host(ctypes.byref(shape), ctypes.byref(rot), (ctypes.c_int64 * 3)(*start), base,
+                                         table.data_ptr() or ctypes.addressof((ctypes.c_float * 1)())))
+    return table
+
+
+def make_rotation(table, split, halves=False) -> Rotation:
+    """table: fp32 [entries, 2] (cos, sin) on the device, of T*split[0] + H*split[1] + W*split[2] entries as rotation_table
+    has them, or [B, entries, 2] for one of each batch element; halves: channel i turns with i + 64 instead of 2i with 2i + 1."""
+    torch = _torch or _import_torch()
+    if table.dtype != torch.float32 or table.dim() not in (2, 3) or table.shape[-1] != 2 or not table.is_contiguous():
+        raise ValueError(f"a rotation's table is contiguous fp32 [entries, 2] or [B, entries, 2], not {table.dtype} {tuple(table.shape)}")
+    rot = Rotation(table.data_ptr(), 2 * table.shape[1] if table.dim() == 3 else 0, *split, PAIRS_HALVES if halves else PAIRS_ADJACENT)
+    rot.tensor = table
+    return rot
+
+
+def _check_turning(shape: Shape, norm, rotation):
+    weight = table = None
+    if norm is not None:
+        weight = norm.tensor
+        if weight is not None and norm.per_head and weight.shape[0] != shape.heads:
+            raise ValueError(f"a norm's weight of {weight.shape[0]} heads, not {shape.heads}")
+    if rotation is not None:
+        table = rotation.tensor
+        n = shape.T * rotation.pairs_t + shape.H * rotation.pairs_h + shape.W * rotation.pairs_w
+        if table.shape[-2] != n or (table.dim() == 3 and table.shape[0] != shape.B):
+            raise ValueError(f"a rotation's table {tuple(table.shape)}, not of {n} entries (of {shape.B} batch elements)")
+    return weight, table
+
+
+def norm_rotate(shape: Shape, x, norm: Norm = None, rotation: Rotation = None, out=None, out_dtype=None):
+    """Each head's norm and the rotation by the token's place.  x: bf16 or fp32 [B, heads, tokens, 128] of any strides, for
+    instance projection.view(B, tokens, heads, 128).transpose(1, 2); out alike (default: raster order, x's type)."""
+    torch = _torch or _import_torch()
+    weight, table = _check_turning(shape, norm, rotation)
+    if out is None:
+        out = torch.empty((shape.B, shape.heads, shape.T, shape.H, shape.W, shape.head_dim), dtype=out_dtype or x.dtype,
+                          device=x.device)
+    _here(x, out, weight, table)
+    _check(lib().fps_norm_rotate(shape, _view(x, "x"), norm, rotation, _view(out, "out"), _stream()))
+    return out
+
+
+def norm_rotate_operand(shape: Shape, x, role, prec=PREC_FP8, norm: Norm = None, rotation: Rotation = None, out=None, scales=None):
+    """norm_rotate straight into the operand of attn_fwd (Q or K).  Returns (packed operand, scales or None)."""
+    torch = _torch or _import_torch()
+    weight, table = _check_turning(shape, norm, rotation)
+    fp8 = prec == PREC_FP8
+    if out is None:
+        out = torch.empty(packed_bytes(shape, prec), dtype=torch.uint8, device=x.device)
+    if not fp8:
+        scales = None
+    elif scales is None:
+        scales = torch.empty((shape.B, shape.heads, num_groups(shape)), dtype=torch.float32, device=x.device)
+    _here(x, out, scales, weight, table)
+    _whole(out, torch.uint8, packed_bytes(shape, prec), "out")
+    if fp8:
+        _whole(scales, torch.float32, shape.B * shape.heads * num_groups(shape), "scales")
+    _check(lib().fps_norm_rotate_operand(shape, _view(x, "x"), norm, rotation, role, prec, out.data_ptr(), _ptr(scales), _stream()))
+    return out, scales
+
+
+def norm_rotate_bwd_bytes(shape: Shape, norm: Norm = None) -> int:
+    n = int(lib().fps_norm_rotate_bwd_bytes(shape, norm))
+    if n == 0:
+        raise FpsError(FPS_ERR_INVALID_ARG, last_error())
+    return n
+
+
+def norm_rotate_bwd(shape: Shape, x, dy, norm: Norm = None, rotation: Rotation = None, dx=None, dweight=None, workspace=None,
+                    need_dweight=True):
+    """Gradient of norm_rotate: (dx, dweight); dweight is None without a weight, or if it is not wanted.  Straight through a
+    quantisation that follows: dy is then the gradient of the operand's values."""
+    torch = _torch or _import_torch()
+    weight, table = _check_turning(shape, norm, rotation)
+    if dx is None:
+        dx = torch.empty_like(x)
+    if weight is None or not need_dweight:
+        dweight = workspace = None
+    else:
+        if dweight is None:
+            dweight = torch.empty_like(weight)
+        _whole(dweight, torch.float32, weight.numel(), "dweight")
+        if workspace is None:
+            workspace = torch.empty(norm_rotate_bwd_bytes(shape, norm), dtype=torch.uint8, device=x.device)
+    _here(x, dy, dx, dweight, workspace, weight, table)
+    _check(lib().fps_norm_rotate_bwd(shape, _view(x, "x"), norm, rotation, _view(dy, "dy"), _view(dx, "dx"), _ptr(dweight),
+                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     _stream()))
+    return dx, dweight
+
+
+def dequantize(shape: Shape, xq, scales, role, vscale=VSCALE_TILE, out=None, out_dtype=None):
+    """The values of a packed E4M3 operand, code * scale, in raster order [B, heads, T, H, W, 128]."""
+    torch = _torch or _import_torch()
+    dims = (shape.B, shape.heads, shape.T, shape.H, shape.W, shape.head_dim)
+    if out is None:
+        out = torch.empty(dims, dtype=out_dtype or torch.bfloat16, device=xq.device)
+    _here(xq, scales, out)
+    _whole(xq, torch.uint8, packed_bytes(shape, PREC_FP8), "xq")
+    _whole(out, out.dtype, shape.B * shape.heads * shape.T * shape.H * shape.W * shape.head_dim, "out")
+    n = shape.head_dim if role == ROLE_V and vscale == VSCALE_CHANNEL else num_groups(shape)
+    _whole(scales, torch.float32, shape.B * shape.heads * n, "scales")
+    _check(lib().fps_dequantize(shape, xq.data_ptr(), scales.data_ptr(), role, vscale, _dtype_code(out), out.data_ptr(), _stream()))
     return out

@@ -1,0 +1,339 @@
+"""Norm and rotation of Q and K, their operands and their gradient, on the GPU against the definitions in 64 bits."""
+import sys
+
+import pytest
+
+from paper_2506_04648_amd import fps
+from tests import operators_plain as op
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def make_tensor(gen, B, heads, N, dt, layout):
+    """[B, heads, N, 128]: in raster order, as a third of a projection's rows, or with gaps between all axes."""
+    if layout == "raster":
+        return torch.randn(B, heads, N, 128, generator=gen, device=DEV).to(dt)
+    if layout == "fused":
+        return torch.randn(B, N, 3, heads, 128, generator=gen, device=DEV).to(dt)[:, :, 1].transpose(1, 2)
+    return torch.randn(B, heads + 1, N + 3, 144, generator=gen, device=DEV).to(dt)[:, 1:, 2:N + 2, 8:136]
+
+
+class Case:
+    def __init__(self, B=1, heads=2, grid=(2, 3, 5), tile=(1, 2, 2), qtile=None, dt=BF16, layout="raster", weight="shared",
+                 split=(22, 21, 21), halves=False, norm=True, rotate=True, start=(0, 0, 0), eps=1e-6, seed=1, tables=1):
+        self.gen = gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.B, self.heads, self.grid, self.N, self.dt, self.halves = B, heads, grid, grid[0] * grid[1] * grid[2], dt, halves
+        self.shape = fps.make_shape(heads, grid, tile, B=B, qtile=qtile)
+        self.x = make_tensor(gen, B, heads, self.N, dt, layout)
+        self.weight = None
+        if weight != "none":
+            self.weight = torch.randn((heads, 128) if weight == "per_head" else (128,), generator=gen, device=DEV)
+        self.norm = fps.make_norm(self.weight, eps) if norm else None
+        self.rotation = turn = None
+        if rotate:
+            table = torch.stack([fps.rotation_table(self.shape, split, start=(start[0] + 7 * b,) + tuple(start[1:])) for b in range(tables)])
+            table = (table if tables > 1 else table[0]).to(DEV)
+            self.rotation = fps.make_rotation(table, split, halves)
+            turn = op.turn_of_tokens(table, grid, split)
+        self.plain = op.Turning(self.weight if norm else None, eps, turn, halves, norm)
+
+
+CASES = [
+    dict(),
+    dict(grid=(1, 1, 1), heads=1),
+    dict(grid=(1, 1, 1), heads=3, B=2, layout="fused", dt=F32, halves=True, start=(1 << 40, 3, -5)),
+    dict(grid=(1, 1, 33), heads=5, weight="per_head", layout="fused"),
+    dict(grid=(3, 7, 9), heads=5, B=2, layout="gaps", halves=True, weight="per_head", tables=2),
+    dict(grid=(3, 7, 9), heads=4, layout="gaps", dt=F32, split=(10, 0, 30)),
+    dict(grid=(5, 23, 37), heads=7, layout="fused", halves=True, weight="none"),
+    dict(grid=(5, 23, 37), heads=6, layout="fused", split=(0, 0, 0)),
+    dict(grid=(2, 5, 31), heads=3, split=(64, 0, 0), start=(100000, 0, 0)),
+    dict(grid=(2, 5, 31), heads=3, norm=False, split=(0, 32, 32), dt=F32),
+    dict(grid=(2, 5, 31), heads=3, rotate=False, dt=F32),
+    dict(grid=(2, 5, 31), heads=3, rotate=False, norm=False, layout="fused"),
+    dict(grid=(9, 40, 64), heads=9, B=1, layout="fused", weight="per_head"),     # more rows than one head a workgroup
+    dict(grid=(9, 40, 64), heads=9, B=2, layout="fused", dt=F32, halves=True),
+]
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_norm_rotate(case, out):
+    say("norm_rotate", case, out)
+    c = Case(**case)
+    want, bound = c.plain.forward(c.x)
+    keep = c.x.clone()
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out_dtype=out)
+    assert y.shape == (c.B, c.heads) + c.grid + (128,)
+    worst = op.within(y.reshape(want.shape), want, bound, out)
+    # into the caller's layout: the same bits, and nothing beside them
+    wide = torch.full((c.B, c.N + 2, c.heads + 1, 136), 7.0, device=DEV, dtype=out)
+    view = wide[:, 1:-1, 1:, :128].transpose(1, 2)
+    assert fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out=view) is view
+    same = torch.equal(view, y.reshape(view.shape))
+    view.fill_(7.0)
+    assert worst <= 1 and same and bool((wide == 7.0).all()) and torch.equal(keep, c.x), worst
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+def test_in_place_on_a_share_of_a_projection(dt):
+    c = Case(grid=(3, 9, 11), heads=4, layout="fused", dt=dt, B=2)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation)
+    assert fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out=c.x) is c.x
+    assert torch.equal(c.x, y.reshape(c.x.shape))
+
+
+def test_rows_with_infinities_and_nans_leave_the_others_alone():
+    c = Case(grid=(2, 5, 31), heads=3)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation).reshape(c.x.shape)
+    bad = c.x.clone()
+    bad[0, 1, 17, 5], bad[0, 2, 18, 127], bad[0, 0, 19, 0] = float("nan"), float("inf"), float("-inf")
+    z = fps.norm_rotate(c.shape, bad, c.norm, c.rotation).reshape(c.x.shape)
+    rows = torch.zeros(c.x.shape[:3], dtype=torch.bool, device=DEV)
+    rows[0, 1, 17] = rows[0, 2, 18] = rows[0, 0, 19] = True
+    assert torch.equal(z[~rows], y[~rows])
+    assert bool((z[rows].isnan() | z[rows].isinf()).any(-1).all())
+    zero = fps.norm_rotate(c.shape, torch.zeros_like(c.x), c.norm, c.rotation)
+    assert bool((zero == 0).all())
+
+
+def test_offsets_beyond_32_bits():
+    """Two batch elements 2^31 + 8 elements apart in bf16, rows of the heads 2^27 apart."""
+    c = Case(grid=(1, 3, 5), heads=3, B=2)
+    far = torch.empty((1 << 31) + 8 + 2 * (1 << 27) + 15 * 128, dtype=BF16, device=DEV)
+    x = far.as_strided((2, 3, 15, 128), ((1 << 31) + 8, 1 << 27, 128, 1))
+    x.copy_(c.x)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation)
+    assert torch.equal(fps.norm_rotate(c.shape, x, c.norm, c.rotation), y)
+    fps.norm_rotate(c.shape, x, c.norm, c.rotation, out=x)
+    assert torch.equal(x.contiguous().reshape(y.shape), y)
+
+
+@pytest.mark.parametrize("start", [(0, 0, 0), (5, 17, 3), (1 << 40, 0, 0)])
+def test_rotation_table(start):
+    """cos and sin of angles in 64 bits, which have 2^-53 of the angle: at 2^40, 2^-13."""
+    shape = fps.make_shape(1, (4, 6, 7), (1, 2, 2))
+    split = (22, 21, 20)
+    table = fps.rotation_table(shape, split, base=500.0, start=start).double()
+    at = 0
+    for n, c, first in zip((4, 6, 7), split, start):
+        place = torch.arange(n, dtype=torch.float64)[:, None] + first
+        angle = place * 500.0 ** (-torch.arange(c, dtype=torch.float64) / c)
+        part = table[at:at + n * c].reshape(n, c, 2)
+        bound = op.F32 + 4 * 2.0 ** -53 * (1 + angle.abs())
+        assert bool(((part[..., 0] - angle.cos()).abs() <= bound).all())
+        assert bool(((part[..., 1] - angle.sin()).abs() <= bound).all())
+        at += n * c
+    assert at == table.shape[0]
+
+
+# ---- operands -----------------------------------------------------------------------------------
+OPERANDS = [
+    dict(grid=(4, 16, 16), tile=(2, 4, 4)),
+    dict(grid=(1, 1, 1), tile=(1, 8, 16), heads=1),
+    dict(grid=(3, 9, 20), tile=(1, 8, 16), layout="fused", halves=True, B=2),
+    dict(grid=(3, 7, 9), tile=(2, 4, 16), layout="gaps", dt=F32, weight="per_head"),          # one block of 128
+    dict(grid=(5, 7, 9), tile=(3, 4, 4), layout="fused", heads=5),                             # two blocks of 32
+    dict(grid=(5, 9, 13), tile=(2, 4, 12), halves=True, dt=F32),                                # three of 32
+    dict(grid=(3, 13, 20), tile=(2, 8, 16), B=2, layout="fused"),                              # two of 128
+    dict(grid=(7, 9, 10), tile=(6, 8, 8), halves=True),                                        # three of 128
+    dict(grid=(5, 18, 33), tile=(4, 16, 16), layout="fused", heads=3),                         # eight of 128: two passes
+    dict(grid=(5, 18, 33), tile=(8, 8, 8), dt=F32, halves=True),                               # four
+    dict(grid=(3, 13, 20), tile=(2, 8, 16), qtile=(1, 8, 8), layout="fused"),
+    dict(grid=(2, 9, 20), tile=(1, 7, 15), weight="none", split=(8, 8, 8)),
+    dict(grid=(3, 9, 20), tile=(1, 8, 16), norm=False, rotate=False, layout="fused"),
+]
+
+
+@pytest.mark.parametrize("case", OPERANDS)
+@pytest.mark.parametrize("role", [fps.ROLE_Q, fps.ROLE_K])
+def test_fp8_operand(case, role):
+    """Scales to fp32's rounding, and every code the one nearest to value / scale (or its neighbour where the quotient's own
+    error reaches the middle between the two)."""
+    say("operand", case, role)
+    c = Case(**case)
+    y, bound = c.plain.forward(c.x)
+    tile, qtile = case["tile"], case.get("qtile")
+    group, n = op.group_of_tokens(c.grid, tile, qtile)
+    group = group.to(DEV)
+    packed, scales = fps.norm_rotate_operand(c.shape, c.x, role, fps.PREC_FP8, c.norm, c.rotation)
+    top = torch.zeros(c.B, c.heads, n, dtype=torch.float64, device=DEV)
+    off = torch.zeros_like(top)
+    index = group.expand(c.B, c.heads, -1)
+    top.scatter_reduce_(2, index, y.abs().amax(-1), "amax")
+    off.scatter_reduce_(2, index, bound.amax(-1), "amax")
+    want = torch.where(top == 0, torch.ones_like(top), top / 448)
+    assert scales.shape == want.shape
+    assert bool(((scales.double() - want).abs() <= off / 448 + 2 * op.F32 * want).all())
+    values = fps.dequantize(c.shape, packed, scales, role, out_dtype=F32).reshape(y.shape).double()
+    s = scales.double().gather(2, index)[..., None]
+    q, code = y / s, values / s                              # value = code * scale, rounded once
+    slack = bound / s + 4 * op.F32 * (q.abs() + 1)
+    step = op.e4m3_half_step((q.abs() + slack).clamp_max(448.0))
+    assert bool(((code - q).abs() <= step + slack).all())
+    # the codes that the debug call has, at every real token, and zero beside them
+    raw = fps.debug_unpack_q8(c.shape, packed, role).view(torch.float8_e4m3fn).float()
+    again = fps.tile_unorder(c.shape, raw).reshape(y.shape).double()
+    assert bool(((again - code).abs() <= 2 * op.F32 * again.abs()).all())
+    assert int((raw != 0).sum()) == int((again != 0).sum())
+    low = fps.dequantize(c.shape, packed, scales, role)
+    assert torch.equal(low.reshape(y.shape), fps.dequantize(c.shape, packed, scales, role, out_dtype=F32).to(BF16).reshape(y.shape))
+
+
+@pytest.mark.parametrize("case", OPERANDS)
+@pytest.mark.parametrize("role", [fps.ROLE_Q, fps.ROLE_K])
+def test_bf16_operand_is_the_packed_bf16_tensor(case, role):
+    say("bf16 operand", case, role)
+    c = Case(**case)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out_dtype=BF16)
+    want, _ = fps.pack_tiles_bf16(c.shape, y, role, raster=True)
+    got, scales = fps.norm_rotate_operand(c.shape, c.x, role, fps.PREC_BF16, c.norm, c.rotation)
+    assert scales is None and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("size", [0.0, 1e-38, 3e-30, 1e17])
+@pytest.mark.parametrize("tile", [(1, 8, 16), (4, 16, 16)])
+def test_scales_of_tiny_and_huge_values(size, tile):
+    """Without a norm the values are the inputs: a scale below the normal range, zeros, and the other end."""
+    c = Case(grid=(5, 18, 33), tile=tile, norm=False, rotate=False, dt=F32)
+    c.x.mul_(size)
+    packed, scales = fps.norm_rotate_operand(c.shape, c.x, fps.ROLE_Q)
+    group, n = op.group_of_tokens(c.grid, tile)
+    index = group.to(DEV).expand(1, c.heads, -1)
+    top = torch.zeros(1, c.heads, n, dtype=torch.float64, device=DEV).scatter_reduce_(2, index, c.x.double().abs().amax(-1), "amax")
+    tiniest = 2.0 ** -149
+    want = torch.where(top == 0, torch.ones_like(top), top / 448)
+    assert bool(((scales.double() - want).abs() <= op.F32 * want + tiniest / 2).all())
+    s = scales.double().gather(2, index)[..., None]
+    values = fps.dequantize(c.shape, packed, scales, fps.ROLE_Q, out_dtype=F32).reshape(c.x.shape).double()
+    q = c.x.double() / s
+    # a scale of few bits is itself off, by up to half of the tiniest number: so is the largest quotient, and it saturates
+    assert bool(((values - c.x.double()).abs() <= s * (op.e4m3_half_step(q.clamp(-448, 448)) + 4 * op.F32 * (q.abs() + 1)
+                                                         + (q.abs() - 448).clamp_min(0)) + tiniest).all())
+
+
+@pytest.mark.parametrize("vscale", [fps.VSCALE_TILE, fps.VSCALE_CHANNEL])
+@pytest.mark.parametrize("tile,qtile", [((1, 8, 16), None), ((3, 4, 4), None), ((4, 16, 16), None), ((2, 8, 16), (1, 8, 8))])
+def test_dequantized_v(tile, qtile, vscale):
+    c = Case(grid=(5, 18, 33), tile=tile, qtile=qtile, B=2, heads=3)
+    packed, scales = fps.quantize_tiles(c.shape, c.x.contiguous(), fps.ROLE_V, vscale=vscale, raster=True)
+    got = fps.dequantize(c.shape, packed, scales, fps.ROLE_V, vscale=vscale, out_dtype=F32).reshape(c.x.shape)
+    codes = fps.debug_unpack_q8(c.shape, packed, fps.ROLE_V).view(torch.float8_e4m3fn).float()
+    codes = fps.tile_unorder(c.shape, codes).reshape(c.x.shape)
+    if vscale == fps.VSCALE_CHANNEL:
+        s = scales[:, :, None, :]
+    else:
+        group, _ = op.group_of_tokens(c.grid, tile, qtile)
+        s = scales.gather(2, group.to(DEV).expand(2, 3, -1))[..., None]
+    assert torch.equal(got, codes * s)
+
+
+# ---- the gradient -------------------------------------------------------------------------------
+@pytest.mark.parametrize("case", CASES)
+def test_gradient(case):
+    say("gradient", case)
+    c = Case(**case)
+    dy = make_tensor(c.gen, c.B, c.heads, c.N, c.dt, "raster")
+    dx64, bound, terms, size = c.plain.backward(c.x, dy)
+    keep = c.x.clone(), dy.clone()
+    dx, dw = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation)
+    assert op.within(dx, dx64, bound, c.dt) <= 1
+    assert torch.equal(keep[0], c.x) and torch.equal(keep[1], dy)
+    if c.norm is None or c.weight is None:
+        assert dw is None
+    else:
+        axes = (0, 2) if c.weight.dim() == 2 else (0, 1, 2)
+        # a sum of n terms in fp32, no deeper than n roundings, each term to 24
+        n = min(c.B * c.N * (1 if c.weight.dim() == 2 else c.heads), 1000)
+        allowed = (24 + n) * op.F32 * size.sum(axes)
+        assert bool(((dw.double() - terms.sum(axes)).abs() <= allowed).all())
+        again = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation)[1]
+        assert torch.equal(dw, again)                        # the order of the sum is fixed
+        alone, none = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation, need_dweight=False)
+        assert none is None and torch.equal(alone, dx)
+    # into other layouts, and in place of x and of dy
+    out = make_tensor(c.gen, c.B, c.heads, c.N, c.dt, "fused")
+    fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation, dx=out)
+    assert torch.equal(out, dx)
+    x = c.x.clone()
+    fps.norm_rotate_bwd(c.shape, x, dy, c.norm, c.rotation, dx=x)
+    assert torch.equal(x, dx.reshape(x.shape))
+    fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation, dx=dy)
+    assert torch.equal(dy, dx.reshape(dy.shape))
+
+
+@pytest.mark.parametrize("case", [dict(grid=(2, 3, 7), dt=F32, halves=True, weight="per_head"), dict(grid=(1, 4, 5), dt=F32, layout="fused")])
+def test_gradient_against_differences(case):
+    """L = sum dy y(x, w): its central differences along a direction, whose own error is what the 64-bit formula's differences at the
+    same step are off, and fp32's of y over the step."""
+    c = Case(**case)
+    dy = make_tensor(c.gen, c.B, c.heads, c.N, c.dt, "raster")
+    d = torch.randn(c.x.shape, generator=c.gen, device=DEV)
+    dw_dir = torch.randn(c.weight.shape, generator=c.gen, device=DEV)
+    dx, dw = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation)
+    h = 2.0 ** -7
+
+    def loss(x, w):
+        y = fps.norm_rotate(c.shape, x, fps.make_norm(w, 1e-6), c.rotation).reshape(dy.shape)
+        plain = op.Turning(w, 1e-6, c.plain.turn, c.halves)
+        y64, bound = plain.forward(x)
+        off = ((bound + op.F32 * y64.abs()) * dy.double().abs()).sum()
+        return float((y.double() * dy.double()).sum()), float((y64 * dy.double()).sum()), float(off)
+
+    dx64, _, terms, _ = c.plain.backward(c.x, dy)
+    dw64 = terms.sum((0, 2) if c.weight.dim() == 2 else (0, 1, 2))
+    for x0, x1, w0, w1, slope, slope64 in (
+            (c.x - h * d, c.x + h * d, c.weight, c.weight, float((dx.double() * d.double()).sum()), float((dx64 * d.double()).sum())),
+            (c.x, c.x, c.weight - h * dw_dir, c.weight + h * dw_dir, float((dw.double() * dw_dir.double()).sum()), float((dw64 * dw_dir.double()).sum()))):
+        lo, lo64, off0 = loss(x0, w0)
+        hi, hi64, off1 = loss(x1, w1)
+        step = float((x1.double() - x0.double()).abs().sum() + (w1.double() - w0.double()).abs().sum()) / float(((x1 - x0) != 0).sum() * d.abs().mean() + ((w1 - w0) != 0).sum() * dw_dir.abs().mean())
+        assert abs(step / (2 * h) - 1) < 0.1
+        curve = abs((hi64 - lo64) / (2 * h) - slope64)
+        assert abs((hi - lo) / (2 * h) - slope) <= curve + (off0 + off1) / (2 * h) + 64 * op.F32 * abs(slope64) + 1e-3 * abs(slope64)
+
+
+# ---- streams and graphs -------------------------------------------------------------------------
+def test_another_stream_and_a_replayed_graph():
+    """Captured once, replayed on new inputs between eager calls, each replay against the eager result."""
+    c = Case(grid=(3, 9, 20), tile=(4, 16, 16), heads=5, layout="fused", weight="per_head")
+    dy = make_tensor(c.gen, c.B, c.heads, c.N, c.dt, "raster")
+    bytes_ = fps.norm_rotate_bwd_bytes(c.shape, c.norm)
+    bufs = dict(y=torch.empty(c.x.shape, dtype=c.dt, device=DEV), p=torch.empty(fps.packed_bytes(c.shape, 1), dtype=torch.uint8, device=DEV),
+                s=torch.empty(1, 5, fps.num_groups(c.shape), device=DEV), v=torch.empty((1, 5) + c.grid + (128,), dtype=BF16, device=DEV),
+                dx=torch.empty_like(c.x), dw=torch.empty_like(c.weight), ws=torch.empty(bytes_, dtype=torch.uint8, device=DEV))
+
+    def step(b):
+        fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out=b["y"])
+        fps.norm_rotate_operand(c.shape, c.x, fps.ROLE_K, fps.PREC_FP8, c.norm, c.rotation, out=b["p"], scales=b["s"])
+        fps.dequantize(c.shape, b["p"], b["s"], fps.ROLE_K, out=b["v"])
+        fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, c.rotation, dx=b["dx"], dweight=b["dw"], workspace=b["ws"])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(bufs)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(bufs)
+    for k in range(4):
+        c.x.copy_(torch.randn(c.x.shape, generator=c.gen, device=DEV))
+        dy.copy_(torch.randn(dy.shape, generator=c.gen, device=DEV))
+        eager = {n: torch.empty_like(t) for n, t in bufs.items()}
+        step(eager)
+        for t in bufs.values():
+            t.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("y", "s", "v", "dx", "dw", "p"):
+            assert torch.equal(eager[n], bufs[n]), (k, n)
