@@ -56,7 +56,7 @@ typedef enum {
     FPS_OK = 0,
     FPS_ERR_INVALID_ARG = -1,   /* null pointer, non-positive dimension, misalignment, bad enum */
     FPS_ERR_UNSUPPORTED = -2,   /* valid request outside the implemented shapes                  */
-    FPS_ERR_WORKSPACE = -3,     /* reserved                                                      */
+    FPS_ERR_WORKSPACE = -3,     /* a workspace is smaller than the call needs                    */
     FPS_ERR_HIP = -4            /* a HIP call or kernel launch failed; text in fps_last_error()  */
 } fps_status;
 
@@ -336,6 +336,40 @@ int fps_norm_rotate_bwd(const fps_shape* shape, const fps_view* x, const fps_nor
  * type dt (device).  Inverse of the operand's layout; `vscale` is ignored for roles Q and K. */
 int fps_dequantize(const fps_shape* shape, const void* xq, const float* scales, fps_role role, fps_vscale vscale,
                    fps_out_dtype dt, void* x_raster, void* stream);
+
+/* ---- products in microscaled 4-bit floating point -----------------------------------------------
+ * A matrix [rows, K] is cut into blocks of 32 along K.  A block's scale is a power of two, 2^e with e = floor(log2 amax) - 2 of its
+ * largest magnitude, at least 2^-127 (2^0 for a block of zeros; NaN for one that holds an infinity or a NaN), kept as the byte
+ * e + 127 (255: NaN); its elements are E2M1 codes of x / 2^e (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign): round-to-nearest-even,
+ * saturating.  17/32 of a byte an element.  The packed form is the library's own (the matrix instructions' operand order), the same
+ * for both operands of a product: a layer's weights are packed once, its rows in every call.
+ *
+ * A view stands for a matrix of B*rows rows and heads*cols columns: column h*cols + c of row b*rows + r is element (b,h,r,c).  So
+ * a plain matrix is B = heads = 1, a projection's result can be written in raster order for the attention, and the attention's
+ * output read in raster order for the next projection.  Views are bf16 or fp32, data is 16-byte aligned and rows start anywhere;
+ * with several heads cols is a multiple of 32. */
+
+/* Bytes of the packed form of a matrix, or 0 if rows or cols is not in 1 .. 2^31 - 1 or it is too large. */
+size_t fps_mx4_bytes(int64_t rows, int64_t cols);
+
+/* x -> packed (device, fps_mx4_bytes of x's matrix). */
+int fps_mx4_quantize(const fps_view* x, void* packed, void* stream);
+
+/* The values of a packed matrix (device) of y's size -> y; exact in both types unless a value is below bf16's normal range. */
+int fps_mx4_dequantize(const void* packed, const fps_view* y, void* stream);
+
+/* y = A B^T + bias: A packed [M,K], B packed [N,K], bias fp32 [N] or NULL (all device), M x N the matrix that y stands for.  Sums in
+ * fp32, in an order that only the sizes determine, rounded once. */
+int fps_mx4_matmul(int64_t K, const void* a, const void* b, const float* bias, const fps_view* y, void* stream);
+
+/* Bytes of workspace of fps_mx4_linear for rows of K elements, or 0 as fps_mx4_bytes. */
+size_t fps_mx4_linear_bytes(int64_t rows, int64_t K);
+
+/* y = x W^T + bias with x [M,K] quantised on the way: fps_mx4_quantize and fps_mx4_matmul in one call, the same values bit for bit.  w: packed
+ * [N,K]; workspace: device memory of fps_mx4_linear_bytes(M, K), free again when the call has run; FPS_ERR_WORKSPACE if it is
+ * smaller.  y must not share memory with x. */
+int fps_mx4_linear(const fps_view* x, const void* w, const float* bias, const fps_view* y, void* workspace,
+                   size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ("fps_host.cpp", "fps_layout.hip", "fps_quantize.hip", "fps_attn.hip",
-           "fps_attn_fp8.hip", "fps_attn_bf16.hip", "fps_issue_mix.hip", "fps_host_operators.cpp", "fps_rotate.hip")
+           "fps_attn_fp8.hip", "fps_attn_bf16.hip", "fps_issue_mix.hip", "fps_host_operators.cpp", "fps_rotate.hip",
+           "fps_mx4.hip")
 OUT = os.path.join(_HERE, "libfps.so")
 
 

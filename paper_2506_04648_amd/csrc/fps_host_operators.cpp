@@ -1,6 +1,6 @@
 // Host side of the operators around the attention: validation of views, norms and rotations, the rotation's
 // table, and the extern "C" entry points.
-#include "fps_internal.h"
+#include "fps_mx4.h"
 
 #include <math.h>
 #include <string.h>
@@ -95,6 +95,17 @@ static int check_tokens(const fps_shape* shape, const fps_view* v, const char* n
     const long long tokens = (long long)shape->T * shape->H * shape->W;
     if (tokens > 0x7FFFFFFF) { set_error("more than 2^31 - 1 tokens"); return FPS_ERR_UNSUPPORTED; }
     return check_view(v, name, shape->B, shape->heads, tokens, kHeadDim, 16, output);
+}
+
+// a view as a matrix of B*rows rows and heads*cols columns
+static int check_matrix(const fps_view* v, const char* name, bool output) {
+    FPS_TRY(check_view(v, name, 0, 0, 0, 0, 1, output));
+    if (v->heads > 1 && v->cols % 32) { set_error("%s has several heads of %d columns, not a multiple of 32", name, v->cols); return FPS_ERR_INVALID_ARG; }
+    if (mx4_bytes((long long)v->B * v->rows, (long long)v->heads * v->cols) == 0) {
+        set_error("%s is too large a matrix", name);
+        return FPS_ERR_UNSUPPORTED;
+    }
+    return FPS_OK;
 }
 
 }  // namespace fps
@@ -200,6 +211,61 @@ int fps_dequantize(const fps_shape* shape, const void* xq, const float* scales, 
     FPS_TRY(check_ptr(x_raster, "x_raster"));
     return launch_dequantize(g, xq, scales, role, role == FPS_ROLE_V && vscale == FPS_VSCALE_CHANNEL, dt == FPS_OUT_F32,
                              x_raster, (hipStream_t)stream);
+}
+
+size_t fps_mx4_bytes(int64_t rows, int64_t cols) {
+    const size_t n = mx4_bytes(rows, cols);
+    if (n == 0) set_error("a matrix of %lld x %lld elements cannot be packed", (long long)rows, (long long)cols);
+    return n;
+}
+
+int fps_mx4_quantize(const fps_view* x, void* packed, void* stream) {
+    FPS_TRY(check_matrix(x, "x", false));
+    FPS_TRY(check_ptr(packed, "packed"));
+    return launch_mx4_quantize(*x, packed, (hipStream_t)stream);
+}
+
+int fps_mx4_dequantize(const void* packed, const fps_view* y, void* stream) {
+    FPS_TRY(check_ptr(packed, "packed"));
+    FPS_TRY(check_matrix(y, "y", true));
+    return launch_mx4_dequantize(packed, *y, (hipStream_t)stream);
+}
+
+static int check_product(int64_t K, const void* b, const char* name, const float* bias, const fps_view* y) {
+    FPS_TRY(check_matrix(y, "y", true));
+    FPS_TRY(check_ptr(b, name));
+    if (bias) FPS_TRY(check_ptr(bias, "bias"));
+    if (mx4_bytes((long long)y->B * y->rows, K) == 0 || mx4_bytes((long long)y->heads * y->cols, K) == 0) {
+        set_error("rows of %lld elements cannot be packed", (long long)K);
+        return FPS_ERR_INVALID_ARG;
+    }
+    return FPS_OK;
+}
+
+int fps_mx4_matmul(int64_t K, const void* a, const void* b, const float* bias, const fps_view* y, void* stream) {
+    FPS_TRY(check_product(K, b, "b", bias, y));
+    FPS_TRY(check_ptr(a, "a"));
+    return launch_mx4_matmul((int)K, a, b, bias, *y, (hipStream_t)stream);
+}
+
+size_t fps_mx4_linear_bytes(int64_t rows, int64_t K) { return fps_mx4_bytes(rows, K); }
+
+int fps_mx4_linear(const fps_view* x, const void* w, const float* bias, const fps_view* y, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+    FPS_TRY(check_matrix(x, "x", false));
+    const int64_t M = (int64_t)x->B * x->rows, K = (int64_t)x->heads * x->cols;
+    FPS_TRY(check_product(K, w, "w", bias, y));
+    if ((int64_t)y->B * y->rows != M) {
+        set_error("y has %lld rows, x %lld", (long long)y->B * y->rows, (long long)M);
+        return FPS_ERR_INVALID_ARG;
+    }
+    FPS_TRY(check_ptr(workspace, "workspace"));
+    if (workspace_bytes < mx4_bytes(M, K)) {
+        set_error("workspace of %zu bytes, %zu needed", workspace_bytes, mx4_bytes(M, K));
+        return FPS_ERR_WORKSPACE;
+    }
+    FPS_TRY(launch_mx4_quantize(*x, workspace, (hipStream_t)stream));
+    return launch_mx4_matmul((int)K, workspace, w, bias, *y, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -201,6 +201,10 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
 int launch_dequantize(const Geom& g, const void* xq, const float* scales, int role, bool per_channel, bool f32, void* out,
                       hipStream_t st);
 
+int launch_mx4_quantize(const fps_view& x, void* packed, hipStream_t st);
+int launch_mx4_dequantize(const void* packed, const fps_view& y, hipStream_t st);
+int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, const fps_view& y, hipStream_t st);
+
 int launch_copy(const void* in, void* out, long long bytes, hipStream_t st);
 int launch_mfma_rate(int workgroups, int iters, float* sink, hipStream_t st);
 int launch_issue_mix(int kind, int nv, int op, int workgroups_per_cu, int workgroups, int iters,

@@ -32,9 +32,10 @@ EXPORTS = ("fps_last_error", "fps_schedule_select", "fps_num_tiles", "fps_num_gr
            "fps_pack_tiles_bf16", "fps_pack_raster_bf16", "fps_debug_unpack_q8", "fps_debug_copy", "fps_debug_scores_q8",
            "fps_debug_scores_block_q8", "fps_debug_mfma_rate", "fps_debug_issue_mix",
            "fps_attn_fwd", "fps_rotation_floats", "fps_rotation_table_host", "fps_norm_rotate", "fps_norm_rotate_operand",
-           "fps_norm_rotate_bwd_bytes", "fps_norm_rotate_bwd", "fps_dequantize")
+           "fps_norm_rotate_bwd_bytes", "fps_norm_rotate_bwd", "fps_dequantize", "fps_mx4_bytes", "fps_mx4_quantize",
+           "fps_mx4_dequantize", "fps_mx4_matmul", "fps_mx4_linear_bytes", "fps_mx4_linear")
 SIZES = ("fps_num_tiles", "fps_num_groups", "fps_tile_slots", "fps_block_slots", "fps_packed_bytes", "fps_rotation_floats",
-         "fps_norm_rotate_bwd_bytes")                      # exports that return a size, 0 for a refusal
+         "fps_norm_rotate_bwd_bytes", "fps_mx4_bytes", "fps_mx4_linear_bytes")                      # exports that return a size, 0 for a refusal
 
 
 class Shape(ctypes.Structure):
@@ -130,6 +131,11 @@ def lib():
         L.fps_norm_rotate_bwd_bytes.argtypes = [shape, norm]
         L.fps_norm_rotate_bwd.argtypes = [shape, view, norm, rot, view, view, vp, vp, ctypes.c_size_t, vp]
         L.fps_dequantize.argtypes = [shape, vp, vp, ip, ip, ip, vp, vp]
+        L.fps_mx4_bytes.argtypes = L.fps_mx4_linear_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
+        L.fps_mx4_quantize.argtypes = [view, vp, vp]
+        L.fps_mx4_dequantize.argtypes = [vp, view, vp]
+        L.fps_mx4_matmul.argtypes = [ctypes.c_int64, vp, vp, vp, view, vp]
+        L.fps_mx4_linear.argtypes = [view, vp, vp, view, vp, ctypes.c_size_t, vp]
         for name in EXPORTS:
             if name != "fps_last_error":
                 getattr(L, name).restype = ctypes.c_size_t if name in SIZES else ctypes.c_int
@@ -535,4 +541,99 @@ def dequantize(shape: Shape, xq, scales, role, vscale=VSCALE_TILE, out=None, out
     n = shape.head_dim if role == ROLE_V and vscale == VSCALE_CHANNEL else num_groups(shape)
     _whole(scales, torch.float32, shape.B * shape.heads * n, "scales")
     _check(lib().fps_dequantize(shape, xq.data_ptr(), scales.data_ptr(), role, vscale, _dtype_code(out), out.data_ptr(), _stream()))
+    return out
+
+
+def _matrix(t, name) -> View:
+    """A matrix [rows, cols], several [B, rows, cols], or a tensor [B, heads, tokens.., cols] whose matrix has B * tokens rows of
+    heads * cols; columns of a row (of a head) are contiguous."""
+    if t.dim() >= 4:
+        return _view(t, name)
+    if t.dim() < 2:
+        raise ValueError(f"{name} must have rows and columns, not {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the columns must be contiguous")
+    B, stride_b = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
+    return View(t.data_ptr(), _dtype_code(t), B, 1, t.shape[-2], t.shape[-1], stride_b, 0, t.stride(-2))
+
+
+def mx4_bytes(rows, cols) -> int:
+    """Bytes of a matrix packed in microscaled 4-bit floating point."""
+    n = int(lib().fps_mx4_bytes(rows, cols))
+    if n == 0:
+        raise FpsError(FPS_ERR_INVALID_ARG, last_error())
+    return n
+
+
+def mx4_linear_bytes(rows, cols) -> int:
+    n = int(lib().fps_mx4_linear_bytes(rows, cols))
+    if n == 0:
+        raise FpsError(FPS_ERR_INVALID_ARG, last_error())
+    return n
+
+
+def mx4_quantize(x, out=None):
+    """bf16 or fp32 rows (see _matrix) -> packed blocks of 32 E2M1 codes with a power of two each."""
+    torch = _torch or _import_torch()
+    v = _matrix(x, "x")
+    n = mx4_bytes(v.B * v.rows, v.heads * v.cols)
+    if out is None:
+        out = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _here(x, out)
+    _whole(out, torch.uint8, n, "out")
+    _check(lib().fps_mx4_quantize(v, out.data_ptr(), _stream()))
+    return out
+
+
+def mx4_dequantize(packed, rows, cols, out=None, out_dtype=None):
+    """The values of a packed matrix [rows, cols], also into a tensor that stands for one."""
+    torch = _torch or _import_torch()
+    if out is None:
+        out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=packed.device)
+    _here(packed, out)
+    v = _matrix(out, "out")
+    if (v.B * v.rows, v.heads * v.cols) != (rows, cols):
+        raise ValueError(f"out {tuple(out.shape)} is not a matrix of {rows} x {cols}")
+    _whole(packed, torch.uint8, mx4_bytes(rows, cols), "packed")
+    _check(lib().fps_mx4_dequantize(packed.data_ptr(), v, _stream()))
+    return out
+
+
+def _product_out(out, out_dtype, rows, cols, device):
+    torch = _torch or _import_torch()
+    if out is None:
+        out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=device)
+    v = _matrix(out, "out")
+    if (v.B * v.rows, v.heads * v.cols) != (rows, cols):
+        raise ValueError(f"out {tuple(out.shape)} is not a matrix of {rows} x {cols}")
+    return out, v
+
+
+def mx4_matmul(a, b, m, n, k, bias=None, out=None, out_dtype=None):
+    """a b^T + bias of packed matrices a [m, k] and b [n, k]; bias: fp32 [n]."""
+    torch = _torch or _import_torch()
+    out, v = _product_out(out, out_dtype, m, n, a.device)
+    _here(a, b, bias, out)
+    _whole(a, torch.uint8, mx4_bytes(m, k), "a")
+    _whole(b, torch.uint8, mx4_bytes(n, k), "b")
+    if bias is not None:
+        _whole(bias, torch.float32, n, "bias")
+    _check(lib().fps_mx4_matmul(k, a.data_ptr(), b.data_ptr(), _ptr(bias), v, _stream()))
+    return out
+
+
+def mx4_linear(x, w, n, bias=None, out=None, out_dtype=None, workspace=None):
+    """x W^T + bias, x (rows as in mx4_quantize) quantised on the way; w: mx4_quantize of the weights [n, k]."""
+    torch = _torch or _import_torch()
+    xv = _matrix(x, "x")
+    m, k = xv.B * xv.rows, xv.heads * xv.cols
+    out, v = _product_out(out, out_dtype, m, n, x.device)
+    if workspace is None:
+        workspace = torch.empty(mx4_linear_bytes(m, k), dtype=torch.uint8, device=x.device)
+    _here(x, w, bias, out, workspace)
+    _whole(w, torch.uint8, mx4_bytes(n, k), "w")
+    if bias is not None:
+        _whole(bias, torch.float32, n, "bias")
+    _check(lib().fps_mx4_linear(xv, w.data_ptr(), _ptr(bias), v, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                _stream()))
     return out

@@ -115,3 +115,36 @@ def group_of_tokens(grid, tile, qtile=None):
         s = s * ns[a] + at[a] % tile[a] // q[a]
     NS = math.prod(ns)
     return (u * NS + s).reshape(-1), math.prod(n) * NS
+
+
+# ---- microscaled 4-bit floating point -----------------------------------------------------------
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def mx4_values(x):
+    """What blocks of 32 along the last axis of x [rows, K] stand for, by the definition: NaN in a block with anything not finite."""
+    rows, K = x.shape
+    b = torch.nn.functional.pad(x.double(), (0, -K % 32)).reshape(rows, -1, 32)
+    top = b.abs().amax(-1, keepdim=True)
+    bad = ~top.isfinite() | b.isnan().any(-1, keepdim=True)
+    e = (torch.frexp(torch.where(bad, 1.0, top)).exponent - 3).clamp_min(-127)       # floor(log2) - 2
+    unit = ((torch.where(top == 0, 0, e).long() + 1023) << 52).view(torch.float64)   # 2^e exactly; ldexp on a GPU is off by a step
+    v = torch.where(bad, 0.0, b) / unit
+    size = v.abs()
+    index = torch.zeros_like(size)
+    for i in range(7):                                       # middles: ties to the even index
+        middle = (E2M1[i] + E2M1[i + 1]) / 2
+        index += (size > middle) if i % 2 == 0 else (size >= middle)
+    level = torch.tensor(E2M1, dtype=torch.float64, device=x.device)[index.long()]
+    out = torch.where(bad, float("nan"), torch.where(v < 0, -level, level) * unit)
+    return out.reshape(rows, -1)[:, :K]
+
+
+def mx4_product(a, b, bias=None):
+    """a [M, K], b [N, K] as values; the product and a bound on what the sums of the matrix instructions may be off: each adds 64
+    products to the sum before it, dropping less than a step (2^-23) of their magnitudes together, and less than 16 partial sums are
+    added at the end."""
+    y, size = a @ b.t(), a.abs() @ b.abs().t()
+    if bias is not None:
+        y, size = y + bias.double(), size + bias.double().abs()
+    return y, (-(-a.shape[1] // 64) + 16) * 2.0 ** -23 * size

@@ -133,3 +133,73 @@ def test_the_binding_refuses():
     assert [getattr(fps._view(six, "x"), n) for n in ("dt", "rows", "stride_h", "stride_r")] == [1, 30, 30 * 128, 128]
     wide = torch.zeros(1, 30, 3, 2, 128)[:, :, 1].transpose(1, 2)
     assert [getattr(fps._view(wide, "x"), n) for n in ("rows", "stride_h", "stride_r")] == [30, 128, 768]
+
+
+# ---- microscaled 4-bit floating point -----------------------------------------------------------
+def matrix(data=GOOD, dt=fps.OUT_BF16, B=1, heads=1, rows=5, cols=70, stride_b=0, stride_h=0, stride_r=71):
+    return fps.View(data, dt, B, heads, rows, cols, stride_b, stride_h, stride_r)
+
+
+def test_packed_sizes():
+    """32 rows by 256 columns are 4352 bytes."""
+    L = fps.lib()
+    for rows, cols, units in ((1, 1, 1), (32, 256, 1), (33, 256, 2), (32, 257, 2), (75600, 5120, 2363 * 20)):
+        assert L.fps_mx4_bytes(rows, cols) == L.fps_mx4_linear_bytes(rows, cols) == 4352 * units
+    for rows, cols in ((0, 5), (5, 0), (-1, 5), (1 << 31, 5), (5, 1 << 31), (1 << 30, 1 << 20)):
+        assert L.fps_mx4_bytes(rows, cols) == 0 and "packed" in fps.last_error()
+        with pytest.raises(fps.FpsError):
+            fps.mx4_bytes(rows, cols)
+
+
+BAD_MATRICES = [None, matrix(data=None), matrix(data=ODD), matrix(dt=2), matrix(rows=0), matrix(cols=0), matrix(stride_r=-1),
+                matrix(heads=2, stride_h=71, stride_r=142), matrix(B=0)]
+BAD_RESULTS = [matrix(stride_r=69), matrix(stride_r=0), matrix(B=2, stride_b=71), matrix(heads=2, cols=32, stride_h=0, stride_r=64)]
+
+
+@pytest.mark.parametrize("i", range(len(BAD_MATRICES) + len(BAD_RESULTS)))
+def test_bad_matrices(i):
+    L, good = fps.lib(), matrix()
+    bad, need = (BAD_MATRICES + BAD_RESULTS)[i], fps.mx4_bytes(5, 70)
+    if i < len(BAD_MATRICES):
+        refused(L.fps_mx4_quantize(bad, GOOD, None))
+        refused(L.fps_mx4_linear(bad, GOOD, None, good, GOOD, need, None))
+    refused(L.fps_mx4_dequantize(GOOD, bad, None))
+    refused(L.fps_mx4_matmul(70, GOOD, GOOD, None, bad, None))
+    refused(L.fps_mx4_linear(good, GOOD, None, bad, GOOD, need, None))
+
+
+def test_the_rest_of_a_products_arguments():
+    L, v = fps.lib(), matrix()
+    need = fps.mx4_bytes(5, 70)
+    big = matrix(rows=1 << 30, cols=1 << 20, stride_r=1 << 20)
+    refused(L.fps_mx4_quantize(big, GOOD, None), fps.FPS_ERR_UNSUPPORTED)
+    for p in (None, ODD):
+        refused(L.fps_mx4_quantize(v, p, None))
+        refused(L.fps_mx4_dequantize(p, v, None))
+        refused(L.fps_mx4_matmul(70, p, GOOD, None, v, None))
+        refused(L.fps_mx4_matmul(70, GOOD, p, None, v, None))
+        refused(L.fps_mx4_linear(v, p, None, v, GOOD, need, None))
+        refused(L.fps_mx4_linear(v, GOOD, None, v, p, need, None))
+    refused(L.fps_mx4_matmul(70, GOOD, GOOD, ODD, v, None))
+    refused(L.fps_mx4_linear(v, GOOD, ODD, v, GOOD, need, None))
+    for K in (0, -1, 1 << 31, 1 << 40):
+        refused(L.fps_mx4_matmul(K, GOOD, GOOD, None, v, None))
+    refused(L.fps_mx4_linear(v, GOOD, None, matrix(rows=6), GOOD, need, None))
+    assert "rows" in fps.last_error()
+    refused(L.fps_mx4_linear(v, GOOD, None, v, GOOD, need - 1, None), fps.FPS_ERR_WORKSPACE)
+
+
+def test_the_binding_refuses_products():
+    x, w = torch.zeros(5, 70), torch.zeros(fps.mx4_bytes(9, 70), dtype=torch.uint8)
+    for call in (lambda: fps.mx4_quantize(x), lambda: fps.mx4_dequantize(w, 9, 70), lambda: fps.mx4_linear(x, w, 9),
+                 lambda: fps.mx4_matmul(w, w, 9, 9, 70)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    for bad in (torch.zeros(70), torch.zeros(70, 5).t(), x.to(torch.float16)):
+        with pytest.raises(ValueError):
+            fps.mx4_quantize(bad)
+    for out in (torch.zeros(5, 8), torch.zeros(6, 9), torch.zeros(1, 3, 5, 32)):
+        with pytest.raises(ValueError, match="not a matrix"):
+            fps.mx4_linear(x, w, 9, out=out)
+    three = torch.zeros(2, 5, 70)[:, 1:]
+    assert [getattr(fps._matrix(three, "x"), n) for n in ("B", "heads", "rows", "cols", "stride_b", "stride_r")] == [2, 1, 4, 70, 350, 70]
