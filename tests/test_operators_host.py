@@ -171,7 +171,7 @@ def test_bad_matrices(i):
 def test_the_rest_of_a_products_arguments():
     L, v = fps.lib(), matrix()
     need = fps.mx4_bytes(5, 70)
-    big = matrix(rows=1 << 30, cols=1 << 20, stride_r=1 << 20)
+    big = matrix(rows=1 << 30, cols=1 << 14, stride_r=1 << 14)
     refused(L.fps_mx4_quantize(big, GOOD, None), fps.FPS_ERR_UNSUPPORTED)
     for p in (None, ODD):
         refused(L.fps_mx4_quantize(v, p, None))
