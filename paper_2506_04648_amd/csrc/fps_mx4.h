@@ -59,4 +59,7 @@ struct Matrix {
     }
 };
 
+// the product of matrices that fill the GPU with 256 x 256 tiles (fps_mx4_matmul.hip)
+int launch_mx4_large(const void* a, const void* b, int K, const float* bias, const fps_view& y, hipStream_t st);
+
 }  // namespace fps
