@@ -37,9 +37,18 @@ struct Matrix {
     long long stride_b, stride_h, stride_r;        // bytes
     int rows, cols, B, heads;
     uint32_t rc_rows, rc_cols;
-    explicit Matrix(const fps_view& v)
-        : data((char*)v.data), rows(v.rows), cols(v.cols), B(v.B), heads(v.heads), rc_rows(reciprocal(v.rows)), rc_cols(reciprocal(v.cols)) {
+    explicit Matrix(const fps_view& v) : data((char*)v.data), rows(v.rows), cols(v.cols), B(v.B), heads(v.heads), rc_cols(reciprocal(v.cols)) {
         const long long e = v.dt == FPS_OUT_F32 ? 4 : 2;
+        if (B > 1 && (rows == 1 || v.stride_b == rows * v.stride_r)) {        // batches that follow each other are one
+            stride_b = 0;
+            stride_r = (rows == 1 ? v.stride_b : v.stride_r) * e;
+            rows *= B;
+            B = 1;
+            stride_h = v.heads > 1 ? v.stride_h * e : 0;
+            rc_rows = reciprocal(rows);
+            return;
+        }
+        rc_rows = reciprocal(rows);
         stride_b = v.B > 1 ? v.stride_b * e : 0;
         stride_h = v.heads > 1 ? v.stride_h * e : 0;
         stride_r = v.rows > 1 ? v.stride_r * e : 0;

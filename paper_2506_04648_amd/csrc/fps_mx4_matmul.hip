@@ -17,6 +17,7 @@ constexpr int kTileEdge = 256, kEdgeTiles = kTileEdge / kMxRows;
 constexpr int kHalf = kMxStepBytes / 2, kSlot = 2 * kEdgeTiles * kHalf, kSlots = 4;              // bytes; of 16 row tiles half a step
 constexpr int kScales = kSlots * kSlot, kScaleSlot = 2 * kEdgeTiles * kMxScaleBytes;               // behind them, two steps' scales
 constexpr int kPieces = kScales + 2 * kScaleSlot;
+constexpr int kBias = kTileEdge * 4;                                       // a tile's bias, for each wave
 constexpr int kPiecePitch = 64 * 2 + 16, kPiece = 32 * kPiecePitch;       // 32 rows of 64 columns in bf16, on their way out
 
 struct TileMap { int tiles_m, tiles_n, total, workgroups; };
@@ -31,6 +32,12 @@ __device__ __forceinline__ void copy_1k(const void* src, uint32_t lane_off, uint
 }
 __device__ __forceinline__ void copy_lanes(const void* src, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "memory", "m0");
+}
+// The lane's number, worked out anew: what follows from it is then not kept in registers where every one is taken
+__device__ __forceinline__ int lane_anew() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
 }
 // Waits until at most N of the wave's copies (and stores) are under way and all it has read from LDS is there; then for the other waves
 template <int N>
@@ -49,9 +56,9 @@ __device__ __forceinline__ Place place_of(const TileMap& t, int i) {
     return Place{8 * g + rem - col * down, col};
 }
 
-template <bool F32>
+template <bool F32, bool HIDDEN>
 __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, TileMap map) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kPieces + 4 * kPiece];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kPieces + 4 * (kPiece + kBias)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, h = lane >> 5;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -142,12 +149,58 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     for (int n = 0; n < 8; ++n) read(0, 0, 0, n);
 #pragma unroll
     for (int i = 0; i < 4; ++i) read_scales(0, i);
-    uint8_t* const piece = lds + kPieces + wave * kPiece;
     const int M = y.all_rows(), N = y.all_cols();
+    // ---- a tile's way out: pieces of 32 rows and 64 (fp32: 32) columns by way of the wave's own part of the LDS, which gives rows of 128 bytes.
+    // A wave's LDS instructions are carried out in their order, so none of this waits for anything but what it reads.
+    constexpr int E = F32 ? 4 : 2, W = 16 / E, JJ = F32 ? 1 : 2;       // bytes an element, elements of a lane's chunk, j of a piece
+    struct Piece { uint8_t* in; const uint8_t* out; int row; };
+    auto piece_of = [&](int l) __attribute__((always_inline)) {
+        uint8_t* const piece = lds + kPieces + wave * kPiece;
+        return Piece{piece + (l & 31) * kPiecePitch + 4 * (l >> 5) * E, piece + (l >> 3) * kPiecePitch + 16 * (l & 7), l >> 3};
+    };
+
+    // HIDDEN: the sums of the tile before, in bf16: registers 8 (4 i + j) + 2 q, + 1 are columns 8 q + 4 h .. of block (i, j)
+    uint32_t sums[HIDDEN ? 128 : 1];
+    int done_rows = 0;                                       // rows of it; there is no tile before the first
+    uint32_t done_at[2];                                     // where the lane's chunk of each 64 columns lies in its row, of the first rows;
+                                                             // all ones, an offset that the store itself drops, outside the matrix
+    auto rows_from = [&](int row) __attribute__((always_inline)) {
+        return __builtin_amdgcn_make_buffer_rsrc(y.data + row * y.stride_r, 0, 0xFFFFFFF0, 0x00027000);
+    };
+    __amdgpu_buffer_rsrc_t done = rows_from(0);
+    const int stride_r = (int)y.stride_r;
+    uint4 chunk[2];
+    auto to_piece = [&](const Piece& at, int k, int n) __attribute__((always_inline)) {           // one of the eight writes of piece k
+        const int i = k >> 1, j = 2 * (k & 1) + (n >> 2), q = n & 3, r = 8 * (4 * i + j) + 2 * q;
+        *reinterpret_cast<uint2*>(at.in + ((n >> 2) * 32 + 8 * q) * 2) = make_uint2(sums[r], sums[r + 1]);
+    };
+    auto from_piece = [&](const Piece& at, int t) __attribute__((always_inline)) { chunk[t & 1] = *reinterpret_cast<const uint4*>(at.out + 8 * t * kPiecePitch); };
+    auto store_chunk = [&](const Piece& at, int k, int t) __attribute__((always_inline)) {        // no branch, which would part the multiplications
+        const int down = 32 * (k >> 1) + 8 * t;
+        const uint32_t outside = (uint32_t)((done_rows - 1 - down - at.row) >> 31);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{chunk[t & 1].x, chunk[t & 1].y, chunk[t & 1].z, chunk[t & 1].w}, done, done_at[k & 1] | outside, down * stride_r, 0);
+    };
+    // What follows multiplication n of 64 of a tile's first step: piece n / 8 is written, and its four chunks are read and, two
+    // multiplications later, stored, two at a time (there are no registers for more)
+    auto way_out = [&](const Piece& at, int n) __attribute__((always_inline)) {
+        const int k = n >> 3, m = n & 7;
+        if (m < 2 && k > 0) store_chunk(at, k - 1, 2 + m);
+        if (m == 6 || m == 7) store_chunk(at, k, m - 6);
+        if (m < 4) { to_piece(at, k, 2 * m); to_piece(at, k, 2 * m + 1); }
+        else from_piece(at, m - 4);
+    };
+    uint8_t* const bias_out = lds + kPieces + 4 * kPiece + wave * kBias;
+    const uint32_t bias_slot = lds0 + kPieces + 4 * kPiece + wave * kBias;
+
     for (; tile < end; tile += stride) {
+        const Place p = place_of(map, tile);
         // The order is as written.  A multiplication takes the matrix unit 32 cycles or more and the wave is alone on its SIMD: what else
         // there is to issue, the operands of the next 64 columns and the copies, stands between the multiplications, one at a time.
-        auto step = [&](bool first) __attribute__((always_inline)) {
+        auto step = [&](auto first_tag) __attribute__((always_inline)) {
+            constexpr bool first = decltype(first_tag)::value, out = HIDDEN && first;
+            Piece at_piece;
+            if (out) at_piece = piece_of(lane_anew());
 #pragma unroll
             for (int i = 0; i < 4; ++i) { sa[i] = sa_next[i]; sb[i] = sb_next[i]; }
             advance();                                       // before all else: behind a branch the multiplications would wait for it
@@ -159,9 +212,16 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
                 for (int n = 0; n < 16; ++n) {
                     multiply(Count<2 * hf>{}, n, first && hf == 0);
                     if (n < 8) read(1, slot, 1, n);
+                    if (out) way_out(at_piece, 32 * hf + n);
+                    if (out && hf == 0 && n == 0) {
+                        const int c = min_of(p.n * kTileEdge + 4 * lane_anew(), N - 4);
+                        copy_lanes((const char*)(bias ? bias : (const float*)b.scales) + (bias ? 4LL * c : 0), bias_slot);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                meet<17>();                                  // the next slot has landed, of two more the copies go on; this one is read
+                // The next slot has landed, of two more the copies go on; this one is read.  Behind the copies that are waited for there
+                // are the bias and the stores of a first step.
+                meet<17 + (out ? (hf ? 23 : 7) : 0)>();
                 auto copying = [&](auto n_tag) __attribute__((always_inline)) {
                     constexpr int n = decltype(n_tag)::value;
                     multiply(Count<2 * hf + 1>{}, n, false);
@@ -169,6 +229,7 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
                     else copy_codes(parity, h_tag, Count<(n & 7)>{});          // of the step after the next, into this slot
                     if (n == 7 && !hf) copy_scales(parity);
                     if (n >= 4 && n < 8 && hf) read_scales(parity ^ 1, n & 3);
+                    if (out) way_out(at_piece, 32 * hf + 16 + n);
                     __builtin_amdgcn_sched_barrier(0);
                 };
                 copying(Count<0>{}); copying(Count<1>{}); copying(Count<2>{}); copying(Count<3>{});
@@ -179,58 +240,98 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
             half(Count<0>{});
             half(Count<1>{});
             parity ^= 1;
+            if (out) {
+#pragma unroll
+                for (int t = 2; t < 4; ++t) store_chunk(at_piece, 7, t);
+            }
         };
-        step(true);
-        for (int s = 1; s < steps; ++s) step(false);
-        // out: pieces of 32 rows and 64 columns by way of the wave's own part of the LDS, rows of 128 bytes
-        const Place p = place_of(map, tile);
+        step(std::true_type{});
+        for (int s = 1; s < steps; ++s) step(std::false_type{});
+
         const int row0 = p.m * kTileEdge + wm * 128, col0 = p.n * kTileEdge + wn * 128;
+        auto biased = [&](int i, int j, int q, float (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * q + k];
+            if (bias) {
+                const int c = col0 + 32 * j + 8 * q + 4 * h;
 #pragma unroll
-            for (int jj = 0; jj < 4; jj += F32 ? 1 : 2) {
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < N) v[k] += bias[c + k];
+            }
+        };
+        if constexpr (HIDDEN) {
+            if (steps == 1) asm volatile("s_waitcnt vmcnt(17)" ::: "memory");        // the bias was copied in this very step
+            const int l = lane_anew();
+            const uint8_t* const bias_at = bias_out + (wn * 128 + 4 * (l >> 5)) * 4;
 #pragma unroll
-                for (int j = jj; j < jj + (F32 ? 1 : 2); ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 4; ++q) {
+                    const float4 read = *reinterpret_cast<const float4*>(bias_at + (32 * j + 8 * q) * 4);
+                    const float add[4] = {bias ? read.x : 0.0f, bias ? read.y : 0.0f, bias ? read.z : 0.0f, bias ? read.w : 0.0f};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
                         float v[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * q + k];
-                        if (bias) {
-                            const int c = col0 + 32 * j + 8 * q + 4 * h;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (c + k < N) v[k] += bias[c + k];
-                        }
-                        uint8_t* const at_piece = piece + (lane & 31) * kPiecePitch + ((j - jj) * 32 + 8 * q + 4 * h) * (F32 ? 4 : 2);
-                        if (F32) *reinterpret_cast<float4*>(at_piece) = make_float4(v[0], v[1], v[2], v[3]);
-                        else *reinterpret_cast<uint2*>(at_piece) =
-                                 make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[0], v[1]}, bf16x2)),
-                                            __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2)));
+                        for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * q + k] + add[k];
+                        const int r = 8 * (4 * i + j) + 2 * q;
+                        sums[r] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[0], v[1]}, bf16x2));
+                        sums[r + 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2));
                     }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);       // the accumulators are read as they are converted
+                }
+            done = rows_from(row0);
+            done_rows = M - row0;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int m = 8 * t + (lane >> 3), c = lane & 7;
-                    const uint4 v = *reinterpret_cast<const uint4*>(piece + m * kPiecePitch + 16 * c);
-                    constexpr int E = F32 ? 4 : 2, W = 16 / E;       // bytes an element, elements a lane
-                    const int row = row0 + 32 * i + m, col = col0 + 32 * jj + W * c;
-                    if (row >= M || col >= N) continue;
-                    char* dst = y.row(row) + y.column<E>(col);
-                    if (col + W <= N) {
-                        __builtin_memcpy(dst, &v, 16);
-                    } else {
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int jj = 0; jj < 2; ++jj) {
+                const int col = col0 + 64 * jj + 8 * (l & 7);
+                done_at[jj] = col < N ? (uint32_t)((l >> 3) * stride_r) + (uint32_t)y.column<2>(col) : 0xFFFFFFFFu;
+            }
+        } else {
+            const Piece at_piece = piece_of(lane);
 #pragma unroll
-                        for (int k = 0; k < W - 1; ++k)
-                            if (col + k < N) {
-                                if (F32) reinterpret_cast<uint32_t*>(dst)[k] = w[k];
-                                else     reinterpret_cast<uint16_t*>(dst)[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
-                            }
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int jj = 0; jj < 4; jj += JJ) {
+#pragma unroll
+                    for (int j = jj; j < jj + JJ; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float v[4];
+                            biased(i, j, q, v);
+                            uint8_t* const at = at_piece.in + ((j - jj) * 32 + 8 * q) * E;
+                            if (F32) *reinterpret_cast<float4*>(at) = make_float4(v[0], v[1], v[2], v[3]);
+                            else *reinterpret_cast<uint2*>(at) =
+                                     make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[0], v[1]}, bf16x2)),
+                                                __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2)));
+                        }
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        from_piece(at_piece, t);
+                        const int row = row0 + 32 * i + 8 * t + (lane >> 3), col = col0 + 32 * jj + W * (lane & 7);
+                        if (row >= M || col >= N) continue;
+                        char* dst = y.row(row) + y.column<E>(col);
+                        if (col + W <= N) {
+                            __builtin_memcpy(dst, &chunk[t & 1], 16);
+                        } else {
+                            const uint32_t w[4] = {chunk[t & 1].x, chunk[t & 1].y, chunk[t & 1].z, chunk[t & 1].w};
+#pragma unroll
+                            for (int k = 0; k < W - 1; ++k)
+                                if (col + k < N) {
+                                    if (F32) reinterpret_cast<uint32_t*>(dst)[k] = w[k];
+                                    else     reinterpret_cast<uint16_t*>(dst)[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                                }
+                        }
                     }
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next piece is written
-            }
+        }
+    }
+    if (HIDDEN) {
+        const Piece at_piece = piece_of(lane);
+#pragma unroll
+        for (int n = 0; n < 64; ++n) way_out(at_piece, n);
+#pragma unroll
+        for (int t = 2; t < 4; ++t) store_chunk(at_piece, 7, t);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // no copy is on its way to LDS that is another workgroup's by then
 }
@@ -245,8 +346,13 @@ int launch_mx4_large(const void* pa, const void* pb, int K, const float* bias, c
     if (total > 0x0FFFFFFF) { set_error("more tiles than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
     map.total = (int)total;
     map.workgroups = 256;
-    if (v.dt == FPS_OUT_F32) mx4_large_kernel<true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-    else                     mx4_large_kernel<false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    // The stores among the next tile's multiplications are of whole 16-byte chunks, at 32-bit offsets from a tile's first row; a
+    // batch whose elements do not follow each other is written between the tiles
+    const bool chunks = y.all_cols() % 8 == 0 && (y.stride_h | y.stride_r) % 16 == 0;
+    const bool near = y.stride_r < (1 << 22) && 128 * y.stride_r + (y.heads - 1) * y.stride_h + 2LL * y.cols < 0xFFFFFFF0LL;
+    if (v.dt == FPS_OUT_F32)                   mx4_large_kernel<true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    else if (y.B == 1 && chunks && near)       mx4_large_kernel<false, true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    else                                       mx4_large_kernel<false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");
 }
