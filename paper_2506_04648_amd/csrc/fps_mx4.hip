@@ -286,7 +286,7 @@ static int launch_direct(const Packed& a, const Packed& b, const float* bias, co
 
 int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, const fps_view& v, hipStream_t st) {
     const Packed pa(a, (long long)v.B * v.rows, K), pb(b, (long long)v.heads * v.cols, K);
-    if ((long long)((pa.tiles + 7) / 8) * ((pb.tiles + 7) / 8) >= 128) return launch_mx4_large(a, b, K, bias, v, st);
+    if (pa.steps < (1 << 22) && (long long)((pa.tiles + 7) / 8) * ((pb.tiles + 7) / 8) >= 128) return launch_mx4_large(a, b, K, bias, v, st);
     if (pa.tiles == 1) return launch_direct<1, 1, 8>(pa, pb, bias, v, st);
     return launch_direct<2, 2, 4>(pa, pb, bias, v, st);
 }

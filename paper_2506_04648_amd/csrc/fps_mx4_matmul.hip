@@ -30,6 +30,9 @@ __device__ __forceinline__ void copy_1k(const void* src, uint32_t lane_off, uint
     asm volatile("s_add_i32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%4"
                  : : "v"(lane_off), "s"(src), "s"(dst), "n"(dst_more - FAR), "n"(FAR) : "memory", "m0", "scc");
 }
+__device__ __forceinline__ void copy_lanes(const void* src, uint32_t lane_off, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(lane_off), "s"(src), "s"(dst) : "memory", "m0");
+}
 __device__ __forceinline__ void copy_lanes(const void* src, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "memory", "m0");
 }
@@ -74,23 +77,27 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     const Packed& mine = wave < 2 ? a : b;
     int copy_tile = tile, copy_step = 0;
     const char* codes_at[4];                                 // of the four row tiles
-    const char* scales_at;                                   // of the lane's share of their scales
+    const char* scales_at;                                   // of their scales,
+    uint32_t scales_off;                                     // the lane's share of which is 16 bytes of tile lane / 16
     auto locate = [&]() __attribute__((always_inline)) {
         const Place p = place_of(map, copy_tile);
         const int first = (wave < 2 ? p.m : p.n) * kEdgeTiles + 4 * (wave & 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i)                          // beyond the last row tile: the last one again
             codes_at[i] = (const char*)mine.codes + (long long)min_of(first + i, mine.tiles - 1) * steps * kMxStepBytes;
-        scales_at = (const char*)mine.scales + (long long)min_of(first + (lane >> 4), mine.tiles - 1) * steps * kMxScaleBytes + 16 * (lane & 15);
+        const int base = min_of(first, mine.tiles - 1);
+        scales_at = (const char*)mine.scales + (long long)base * steps * kMxScaleBytes;
+        scales_off = (uint32_t)(min_of(first + (lane >> 4), mine.tiles - 1) - base) * steps * kMxScaleBytes + 16 * (lane & 15);
     };
     locate();
-    const uint32_t lane_off = 16 * lane, code_slots = lds0 + 4 * wave * kHalf, scale_slots = lds0 + kScales + 4 * wave * kMxScaleBytes;
+    uint32_t lane_off = 16 * lane;
+    const uint32_t code_slots = lds0 + 4 * wave * kHalf, scale_slots = lds0 + kScales + 4 * wave * kMxScaleBytes;
     // one of the eight copies of half a step: kilobyte n % 2 of row tile n / 2; par: parity of the step
     auto copy_codes = [&](int par, auto half_tag, auto n_tag) __attribute__((always_inline)) {
         constexpr int half = decltype(half_tag)::value, n = decltype(n_tag)::value, far = half * kHalf + (n & 1) * 1024;
         copy_1k<far>(codes_at[n >> 1], lane_off, code_slots + par * (2 * kSlot), half * kSlot + (n >> 1) * kHalf + (n & 1) * 1024);
     };
-    auto copy_scales = [&](int par) __attribute__((always_inline)) { copy_lanes(scales_at, scale_slots + par * kScaleSlot); };
+    auto copy_scales = [&](int par) __attribute__((always_inline)) { copy_lanes(scales_at, scales_off, scale_slots + par * kScaleSlot); };
     // to the next step; behind the last tile of the result the last one's again, or what follows it, which nobody reads
     auto advance = [&]() __attribute__((always_inline)) {
         const bool more = ++copy_step < steps;
@@ -107,10 +114,14 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
 
     uint4 ca[2][4], cb[2][4];
     uint32_t sa[4], sb[4], sa_next[4], sb_next[4];
-    const uint8_t* const read_a = lds + 4 * wm * kHalf + 16 * lane;
-    const uint8_t* const read_b = lds + (kEdgeTiles + 4 * wn) * kHalf + 16 * lane;
-    const uint8_t* const read_sa = lds + kScales + 4 * wm * kMxScaleBytes + 4 * lane;
-    const uint8_t* const read_sb = lds + kScales + (kEdgeTiles + 4 * wn) * kMxScaleBytes + 4 * lane;
+    const uint8_t *read_a, *read_b, *read_sa, *read_sb;
+    auto read_by = [&](int l) __attribute__((always_inline)) {
+        read_a = lds + 4 * wm * kHalf + 16 * l;
+        read_b = lds + (kEdgeTiles + 4 * wn) * kHalf + 16 * l;
+        read_sa = lds + kScales + 4 * wm * kMxScaleBytes + 4 * l;
+        read_sb = lds + kScales + (kEdgeTiles + 4 * wn) * kMxScaleBytes + 4 * l;
+    };
+    read_by(lane);
     // one of the eight operands of quarter q (0 or 1) of a slot, in the order of their use
     auto read = [&](int set, int slot, int q, int n) __attribute__((always_inline)) {
         const int at_slot = slot * kSlot + q * 1024;
@@ -194,6 +205,9 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     const uint32_t bias_slot = lds0 + kPieces + 4 * kPiece + wave * kBias;
 
     for (; tile < end; tile += stride) {
+        const int l0 = lane_anew();
+        read_by(l0);
+        lane_off = 16 * l0;
         const Place p = place_of(map, tile);
         // The order is as written.  A multiplication takes the matrix unit 32 cycles or more and the wave is alone on its SIMD: what else
         // there is to issue, the operands of the next 64 columns and the copies, stands between the multiplications, one at a time.
