@@ -83,17 +83,15 @@ __device__ __forceinline__ void store_pairs(char* row, int u, const Pairs& p) {
 
 // Cosines and sines of the unit's pairs 8u..8u+7 for token (t,h,w); pairs that do not turn: (1, 0)
 struct Turn { float c[8], s[8]; };
-__device__ __forceinline__ Turn load_turn(const Turning& k, int b, int t, int h, int w, int u) {
-    Turn r;
+__device__ __forceinline__ Turn load_turn(const Turning& k, const float2* table, int T, int H, int t, int h, int w, int u) {
+    Turn r;                                                  // from a table of T places and H places before those of w
 #pragma unroll
     for (int i = 0; i < 8; ++i) { r.c[i] = 1.0f; r.s[i] = 0.0f; }
-    if (!k.table) return r;
-    const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
-    const int at_t = t * k.ct, at_h = k.T * k.ct + h * k.ch - k.ct, at_w = k.T * k.ct + k.H * k.ch + w * k.cw - k.ct - k.ch;
+    const int at_t = t * k.ct, at_h = T * k.ct + h * k.ch - k.ct, at_w = T * k.ct + H * k.ch + w * k.cw - k.ct - k.ch;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int p = 8 * u + i;
-        if (p < k.ct + k.ch + k.cw) {
+        if (p < k.ct + k.ch + k.cw) {                        // none without a rotation
             const float2 cs = table[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
             r.c[i] = cs.x;
             r.s[i] = cs.y;
@@ -103,7 +101,7 @@ __device__ __forceinline__ Turn load_turn(const Turning& k, int b, int t, int h,
 }
 __device__ __forceinline__ Turn load_turn_of_token(const Turning& k, int b, int n, int u) {
     const int t = quotient(n, k.H * k.W, k.rc_plane), rem = n - t * (k.H * k.W), h = quotient(rem, k.W, k.rc_row);
-    return load_turn(k, b, t, h, rem - h * k.W, u);
+    return load_turn(k, reinterpret_cast<const float2*>(k.table + b * k.table_b), k.T, k.H, t, h, rem - h * k.W, u);
 }
 template <bool HALVES>
 __device__ __forceinline__ Pairs load_weight(const Turning& k, int h, int u) {
@@ -168,13 +166,16 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // As quantize_tiles_kernel (and pack_bf16_kernel): a workgroup is one scale group of up to three blocks, held in
 // registers from the reading to the encoding; of larger groups a block, of which PASS 0 finds the maximum and PASS 1, which
 // reads x again, encodes.
-constexpr int kWhole = -1;
+// A token's cosines and sines would be four times as many load instructions as its channels: where the entries of the
+// group's planes, rows and columns are at most kStaged they are brought into LDS first.
+constexpr int kWhole = -1, kStaged = 1024;
 template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
                                                                            float* __restrict__ scales, int role, Geom g,
                                                                            int heads) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
     __shared__ uint32_t red[WAVES];
+    __shared__ float2 staged[kStaged];
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     const int blk = blockIdx.x * NB + kb;
     const BlockOrigin org = block_origin(g, blockIdx.x * NB);
@@ -183,20 +184,34 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
     const Pairs weight = load_weight<HALVES>(k, head, u);
 
     Chunks<IN32> in[U];
-    int token[U];                                            // -1: padding
+    Offset token[U];                                         // from the group's first; t < 0: padding
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int slot = org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i;
-        const Offset d = real_token(org.box, slot);
-        token[i] = slot < org.box.n ? n0 + (d.t * g.H + d.h) * g.W + d.w : -1;
-        if (token[i] >= 0) in[i] = load_pairs<IN32, HALVES>(x.at(b, head, token[i]), u);
+        token[i] = real_token(org.box, slot);
+        if (slot < org.box.n) in[i] = load_pairs<IN32, HALVES>(x.at(b, head, n0 + (token[i].t * g.H + token[i].h) * g.W + token[i].w), u);
+        else                  token[i].t = -1;
     }
+    // the group's entries: its planes', rows' and columns' are three runs of the table
+    const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
+    const int et = org.box.n ? real_token(org.box, org.box.n - 1).t + 1 : 0, of_t = et * k.ct, of_h = org.box.eh * k.ch, of_w = org.box.ew * k.cw;
+    const bool in_lds = of_t + of_h + of_w <= kStaged;
+    const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
+    if (k.table && in_lds && et > 0) {
+        for (int i = threadIdx.x; i < of_t + of_h + of_w; i += THREADS * NB)
+            staged[i] = table[i < of_t ? t0 * k.ct + i
+                                       : i < of_t + of_h ? g.T * k.ct + h0 * k.ch + i - of_t : g.T * k.ct + g.H * k.ch + w0 * k.cw + i - of_t - of_h];
+    }
+    __syncthreads();
     Pairs y[U];
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        if (token[i] >= 0) {
-            y[i] = norm_rotated(k, unpack<IN32, HALVES>(in[i]), weight, load_turn_of_token(k, b, token[i], u));
+        if (token[i].t >= 0) {
+            const Offset d = token[i];
+            const Turn turn = in_lds ? load_turn(k, staged, et, org.box.eh, d.t, d.h, d.w, u)
+                                     : load_turn(k, table, g.T, g.H, t0 + d.t, h0 + d.h, w0 + d.w, u);
+            y[i] = norm_rotated(k, unpack<IN32, HALVES>(in[i]), weight, turn);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
@@ -276,50 +291,60 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 }
 
 // ---- the gradient -------------------------------------------------------------------------------
-// A workgroup takes 32 rows at a time, of one head if the heads have weights of their own, and keeps its lanes' share of
-// dweight in registers from row to row; the workgroups' sums are added up by a second kernel, in a fixed order.
-template <bool F32, bool HALVES>
+// A workgroup takes 32 tokens at a time of HC heads (of one head, always the same, if they have weights of their own), reads the rows of all
+// of them at once and their cosines and sines once, and keeps its lanes' share of dweight in registers; the workgroups' sums are
+// added up by a second kernel, in a fixed order.
+template <bool F32, bool HALVES, int HC>
 __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, Rows dx, Turning k, float* __restrict__ partial,
                                                               int tokens, int heads, int batches, int workgroups) {
     __shared__ float red[4][128];
     const int u = threadIdx.x & 7, row = threadIdx.x >> 3, parts = (int)((tokens + 31u) >> 5);
-    // items: (batch, token part) of one head, or (batch, token part, head)
     const int group = blockIdx.x / workgroups, first = blockIdx.x - group * workgroups;
-    const int own_head = k.weight_head ? group : -1, per = own_head >= 0 ? 1 : heads;
-    const long long items = (long long)batches * parts * per;
+    const int own_head = k.weight_head ? group : -1, per = own_head >= 0 ? 1 : (heads + HC - 1) / HC;
+    const long long items = (long long)batches * parts * per;               // (batch, token part, heads)
     Pairs dw;
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw.a[i] = dw.b[i] = 0.0f;
     for (long long item = first; item < items; item += workgroups) {
         const long long bp = item / per;
-        const int h = own_head >= 0 ? own_head : (int)(item - bp * per), b = (int)(bp / parts);
-        const int n = (int)(bp - (long long)b * parts) * 32 + row;
+        const int h0 = own_head >= 0 ? own_head : (int)(item - bp * per) * HC, b = (int)(bp / parts);
+        const int n = (int)(bp - (long long)b * parts) * 32 + row, last = own_head >= 0 ? h0 + 1 : heads;
         if (n >= tokens) continue;
-        const Pairs xv = unpack<F32, HALVES>(load_pairs<F32, HALVES>(x.at(b, h, n), u));
-        const Pairs g0 = unpack<F32, HALVES>(load_pairs<F32, HALVES>(dy.at(b, h, n), u));
+        Chunks<F32> cx[HC], cy[HC];
+#pragma unroll
+        for (int i = 0; i < HC; ++i)
+            if (h0 + i < last) {
+                cx[i] = load_pairs<F32, HALVES>(x.at(b, h0 + i, n), u);
+                cy[i] = load_pairs<F32, HALVES>(dy.at(b, h0 + i, n), u);
+            }
         const Turn turn = load_turn_of_token(k, b, n, u);
-        const Pairs w = load_weight<HALVES>(k, h, u);
-        const float r = inverse_rms(k, xv);
-        Pairs g;
-        float dot = 0.0f;
+        const Pairs w = load_weight<HALVES>(k, h0, u);                       // of all of them, or of the one
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float ga = __builtin_fmaf(g0.a[i], turn.c[i], g0.b[i] * turn.s[i]);
-            const float gb = __builtin_fmaf(g0.b[i], turn.c[i], -(g0.a[i] * turn.s[i]));
-            dw.a[i] = __builtin_fmaf(ga, xv.a[i] * r, dw.a[i]);
-            dw.b[i] = __builtin_fmaf(gb, xv.b[i] * r, dw.b[i]);
-            g.a[i] = ga * w.a[i];
-            g.b[i] = gb * w.b[i];
-            dot = __builtin_fmaf(g.a[i], xv.a[i], __builtin_fmaf(g.b[i], xv.b[i], dot));
-        }
-        const float back = k.norm ? row_sum(dot) * (1.0f / 128.0f) * r * r : 0.0f;
-        Pairs d;
+        for (int i = 0; i < HC; ++i) {
+            if (h0 + i >= last) break;
+            const Pairs xv = unpack<F32, HALVES>(cx[i]), g0 = unpack<F32, HALVES>(cy[i]);
+            const float r = inverse_rms(k, xv);
+            Pairs g;
+            float dot = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            d.a[i] = r * __builtin_fmaf(-xv.a[i], back, g.a[i]);
-            d.b[i] = r * __builtin_fmaf(-xv.b[i], back, g.b[i]);
+            for (int m = 0; m < 8; ++m) {
+                const float ga = __builtin_fmaf(g0.a[m], turn.c[m], g0.b[m] * turn.s[m]);
+                const float gb = __builtin_fmaf(g0.b[m], turn.c[m], -(g0.a[m] * turn.s[m]));
+                dw.a[m] = __builtin_fmaf(ga, xv.a[m] * r, dw.a[m]);
+                dw.b[m] = __builtin_fmaf(gb, xv.b[m] * r, dw.b[m]);
+                g.a[m] = ga * w.a[m];
+                g.b[m] = gb * w.b[m];
+                dot = __builtin_fmaf(g.a[m], xv.a[m], __builtin_fmaf(g.b[m], xv.b[m], dot));
+            }
+            const float back = k.norm ? row_sum(dot) * (1.0f / 128.0f) * r * r : 0.0f;
+            Pairs d;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                d.a[m] = r * __builtin_fmaf(-xv.a[m], back, g.a[m]);
+                d.b[m] = r * __builtin_fmaf(-xv.b[m], back, g.b[m]);
+            }
+            store_pairs<F32, HALVES>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
         }
-        store_pairs<F32, HALVES>(const_cast<char*>(dx.at(b, h, n)), u, d);
     }
     if (!partial) return;
 #pragma unroll
@@ -341,62 +366,91 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
         partial[(long long)blockIdx.x * 128 + c] = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
     }
 }
-__global__ __launch_bounds__(1024) void sum_partials_kernel(const float* __restrict__ partial, float* __restrict__ out, int n) {
-    __shared__ float red[8][128];
-    const int c = threadIdx.x & 127, slice = threadIdx.x >> 7;
-    const float* p = partial + (long long)blockIdx.x * n * 128 + c;
+// Eight channels a workgroup, 32 slices of the n partial sums
+__global__ __launch_bounds__(256) void sum_partials_kernel(const float* __restrict__ partial, float* __restrict__ out, int n) {
+    __shared__ float red[32][9];
+    const int c = threadIdx.x & 7, slice = threadIdx.x >> 3, group = blockIdx.x >> 4, c0 = 8 * (blockIdx.x & 15);
+    const float* p = partial + (long long)group * n * 128 + c0 + c;
     float s = 0.0f;
-    for (int i = slice; i < n; i += 8) s += p[(long long)i * 128];
+#pragma unroll 8
+    for (int i = slice; i < n; i += 32) s += p[(long long)i * 128];
     red[slice][c] = s;
     __syncthreads();
-    if (slice == 0) {
+    if (threadIdx.x < 8) {
+        float t = 0.0f;
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += red[i][c];
-        out[blockIdx.x * 128 + c] = s;
+        for (int i = 0; i < 32; ++i) t += red[i][threadIdx.x];
+        out[group * 128 + c0 + threadIdx.x] = t;
     }
 }
 
 // ---- the values of packed E4M3 operands ---------------------------------------------------------
-// A workgroup takes a block of BS slots: eight lanes a token, 16 codes each.  V's block is turned back in LDS first.
-template <int BS, bool F32>
+// A workgroup takes a block of BS slots: sixteen lanes a token, 8 codes each, so that a row of bf16 is one store of its lanes; all of
+// a thread's codes are requested at once.  V's block is turned back in LDS first.
+template <int BS, bool F32, bool V>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t* __restrict__ xq, const float* __restrict__ scales,
                                                          int role, int per_channel, char* __restrict__ out, Geom g) {
-    __shared__ __attribute__((aligned(16))) uint8_t stage[BS * 128];
+    constexpr int U = BS * 16 / 256;                         // 8-byte units a thread
+    __shared__ __attribute__((aligned(16))) uint8_t stage[V ? BS * 128 : 16];
     const BlockOrigin org = block_origin(g, blockIdx.x);
-    const uint4* src = reinterpret_cast<const uint4*>(xq + (long long)blockIdx.x * (BS * 128));
-    if (role == FPS_ROLE_V) {
-        for (int c = threadIdx.x; c < BS * 8; c += 256) {
-            const int lane = c & 63, db = (c >> 6) & 3, kb = c >> 8, h = lane >> 5, n = lane & 31;
+    const uint8_t* src = xq + (long long)blockIdx.x * (BS * 128);
+    const int c8 = threadIdx.x & 15;
+    uint2 codes[U];
+    if (V) {
+        uint4 v[(U + 1) / 2];
+#pragma unroll
+        for (int i = 0; i < (U + 1) / 2; ++i) {
+            const int c = threadIdx.x + 256 * i;
+            if (c < BS * 8) v[i] = reinterpret_cast<const uint4*>(src)[c];
+        }
+#pragma unroll
+        for (int i = 0; i < (U + 1) / 2; ++i) {
+            const int c = threadIdx.x + 256 * i, lane = c & 63, db = (c >> 6) & 3, kb = c >> 8, h = lane >> 5, n = lane & 31;
+            if (c >= BS * 8) break;
             union { uint4 v; uint8_t b[16]; } o;
-            o.v = src[c];
+            o.v = v[i];
 #pragma unroll
             for (int jj = 0; jj < 16; ++jj) stage[(32 * kb + 8 * (jj >> 2) + 4 * h + (jj & 3)) * 128 + 32 * db + n] = o.b[jj];
         }
         __syncthreads();
     }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int j = (threadIdx.x >> 4) + 16 * i, c16 = c8 >> 1;
+        int at = j * 8 + c16;                                // 16-byte chunk of the block
+        if (!V && role == FPS_ROLE_K) at = (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31);
+        codes[i] = *reinterpret_cast<const uint2*>((V ? stage : src) + 16 * at + 8 * (c8 & 1));
+    }
     const int bh = quotient((int)org.tile_lin, g.M, g.rc_m);
-    const float of_group = per_channel ? 1.0f : scales[quotient(blockIdx.x, g.KBS, g.rc_kbs)];
-    for (int unit = threadIdx.x; unit < BS * 8; unit += 256) {
-        const int j = unit >> 3, c16 = unit & 7, slot = org.slot0 + j;
-        if (slot >= org.box.n) continue;
+    float s[8];
+    if (V && per_channel) {
+        const float4 lo = reinterpret_cast<const float4*>(scales + bh * 128)[2 * c8], hi = reinterpret_cast<const float4*>(scales + bh * 128)[2 * c8 + 1];
+        s[0] = lo.x; s[1] = lo.y; s[2] = lo.z; s[3] = lo.w; s[4] = hi.x; s[5] = hi.y; s[6] = hi.z; s[7] = hi.w;
+    } else {
+        const float of_group = scales[quotient(blockIdx.x, g.KBS, g.rc_kbs)];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] = of_group;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int slot = org.slot0 + (threadIdx.x >> 4) + 16 * i;
+        if (slot >= org.box.n) break;
         const Offset d = real_token(org.box, slot);
-        uint4 codes;
-        if (role == FPS_ROLE_V) codes = reinterpret_cast<const uint4*>(stage)[unit];
-        else codes = src[role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : unit];
-        const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-        float f[16];
+        float f[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-            f[4 * i] = lo[0]; f[4 * i + 1] = lo[1]; f[4 * i + 2] = hi[0]; f[4 * i + 3] = hi[1];
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t w = k ? codes[i].y : codes[i].x;
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+            f[4 * k] = lo[0] * s[4 * k];         f[4 * k + 1] = lo[1] * s[4 * k + 1];
+            f[4 * k + 2] = hi[0] * s[4 * k + 2]; f[4 * k + 3] = hi[1] * s[4 * k + 3];
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] *= per_channel ? scales[bh * 128 + c16 * 16 + i] : of_group;
-        char* row = out + (org.raster0 + ((long long)d.t * g.H + d.h) * g.W + d.w) * (F32 ? 512 : 256);
-        Pairs p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { p.a[i] = f[2 * i]; p.b[i] = f[2 * i + 1]; }
-        store_pairs<F32, false>(row, c16, p);
+        char* dst = out + (org.raster0 + ((long long)d.t * g.H + d.h) * g.W + d.w) * (F32 ? 512 : 256) + c8 * (F32 ? 32 : 16);
+        if (F32) {
+            reinterpret_cast<float4*>(dst)[0] = make_float4(f[0], f[1], f[2], f[3]);
+            reinterpret_cast<float4*>(dst)[1] = make_float4(f[4], f[5], f[6], f[7]);
+        } else {
+            *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+        }
     }
 }
 
@@ -424,6 +478,8 @@ static Turning turning_of(const Geom& g, const fps_norm* norm, const fps_rotatio
     return k;
 }
 static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_PAIRS_HALVES; }
+
+constexpr int kBwdHeads = 4;
 
 // f(bool constants...) for run-time truth values
 template <typename F> static void with(bool a, F&& f) { if (a) f(std::true_type{}); else f(std::false_type{}); }
@@ -483,7 +539,7 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
 // Workgroups of the gradient for each head, or for all where they share a weight
 static int bwd_workgroups(const Geom& g, int heads, bool per_head) {
     const int batches = g.BH / heads;
-    const long long parts = ((long long)g.T * g.H * g.W + 31) / 32, items = parts * batches * (per_head ? 1 : heads);
+    const long long parts = ((long long)g.T * g.H * g.W + 31) / 32, items = parts * batches * (per_head ? 1 : (heads + kBwdHeads - 1) / kBwdHeads);
     const long long most = per_head ? (1024 + heads - 1) / heads : 1024;
     return (int)(items < most ? items : most);
 }
@@ -496,11 +552,11 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
     const bool per_head = norm && norm->per_head && norm->weight;
     const int n = bwd_workgroups(g, x.heads, per_head), sums = per_head ? x.heads : 1;
     if (!dweight) partial = nullptr;
-    with(x.dt == FPS_OUT_F32, [&](auto f32) { with(halves(rot), [&](auto hv) {
-        norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value>
+    with(x.dt == FPS_OUT_F32, [&](auto f32) { with(halves(rot), [&](auto hv) { with(per_head, [&](auto one) {
+        norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value, decltype(one)::value ? 1 : kBwdHeads>
             <<<n * sums, 256, 0, st>>>(rows_of(x), rows_of(dy), rows_of(dx), k, partial, x.rows, x.heads, x.B, n);
-    }); });
-    if (dweight) sum_partials_kernel<<<sums, 1024, 0, st>>>(partial, dweight, n);
+    }); }); });
+    if (dweight) sum_partials_kernel<<<16 * sums, 256, 0, st>>>(partial, dweight, n);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_bwd launch");
 }
@@ -508,10 +564,10 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
 int launch_dequantize(const Geom& g, const void* xq, const float* scales, int role, bool per_channel, bool f32, void* out,
                       hipStream_t st) {
     const int blocks = g.BH * g.M * g.KB;
-    with(g.BS == 128, [&](auto big) { with(f32, [&](auto f) {
-        dequantize_kernel<decltype(big)::value ? 128 : 32, decltype(f)::value>
+    with(g.BS == 128, [&](auto big) { with(f32, [&](auto f) { with(role == FPS_ROLE_V, [&](auto v) {
+        dequantize_kernel<decltype(big)::value ? 128 : 32, decltype(f)::value, decltype(v)::value>
             <<<blocks, 256, 0, st>>>((const uint8_t*)xq, scales, role, per_channel, (char*)out, g);
-    }); });
+    }); }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "dequantize launch");
 }
