@@ -5,7 +5,7 @@
 //   g = R^T dy,  dw = sum g x r,  dx = r (g w - x r^2 mean(g w x))
 //
 // All of it is bound by HBM: some ten operations an element.  Eight lanes hold a row of 128 channels, 16 channels or 8
-// pairs each, so that a row is one 16-byte load (two, four) of each lane, the sum over it three exchanges between neighbouring
+// pairs each, so that a row is two (four) 16-byte loads of each lane, the sum over it three exchanges between neighbouring
 // lanes, and a pair never leaves its lane.  The rotation's tables are as long as the axes: 20 KB at 720p, read from the caches.
 #include "fps_device_common.h"
 
@@ -40,57 +40,74 @@ struct Turning {
     uint32_t rc_plane, rc_row;       // reciprocals of H*W and W
 };
 
-// 8 pairs of channels of a row: unit u of 8.  Adjacent pairs: channels 16u..16u+15; halves: 8u..8u+7 and those + 64.
+// The 16 channels of lane u of the eight that hold a row, so that each load and store of theirs is a run of 64 or 128 bytes: slot s is
+// channel 64 (s / 8) + 8u + s % 8, or, BY4 (fp32 input), 32 (s / 4) + 4u + s % 4.  Pair i of 8: slots 2i and 2i + 1, or, halves,
+// i and i + 8.  (Sixteen channels in a row to a lane, every load half of each line: 720p 350 us instead of 320, the gradient of
+// 480p 70 instead of 61.)
 struct Pairs { float a[8], b[8]; };
-template <bool F32> struct Chunks { uint4 v[F32 ? 4 : 2]; };
-
-template <bool F32, bool HALVES>
-__device__ __forceinline__ Chunks<F32> load_pairs(const char* row, int u) {
-    constexpr int N = F32 ? 4 : 2, E = F32 ? 4 : 2;         // 16-byte loads; bytes an element
-    Chunks<F32> c;
-    const char* p = row + u * (HALVES ? 8 * E : 16 * E);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        c.v[i] = *reinterpret_cast<const uint4*>(p + (HALVES ? (i % (N / 2)) * 16 + (i / (N / 2)) * 64 * E : 16 * i));
-    return c;
+template <bool BY4> __device__ __forceinline__ int channel_of(int u, int s) { return BY4 ? 32 * (s >> 2) + 4 * u + (s & 3) : 64 * (s >> 3) + 8 * u + (s & 7); }
+template <bool BY4, bool HALVES> __device__ __forceinline__ int pair_of(int u, int i) {
+    return HALVES ? channel_of<BY4>(u, i) : channel_of<BY4>(u, 2 * i) >> 1;
 }
-template <bool F32, bool HALVES>
-__device__ __forceinline__ Pairs unpack(const Chunks<F32>& c) {
+template <bool HALVES> __device__ __forceinline__ Pairs as_pairs(const float (&f)[16]) {
     Pairs p;
-    float f[16];
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(c.v);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = F32 ? __uint_as_float(w[i]) : (i & 1) ? high_bf16(w[i >> 1]) : low_bf16(w[i >> 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) { p.a[i] = f[HALVES ? i : 2 * i]; p.b[i] = f[HALVES ? 8 + i : 2 * i + 1]; }
     return p;
 }
-template <bool F32, bool HALVES>
-__device__ __forceinline__ void store_pairs(char* row, int u, const Pairs& p) {
-    constexpr int N = F32 ? 4 : 2, E = F32 ? 4 : 2;
-    float f[16];
+template <bool HALVES> __device__ __forceinline__ void as_slots(const Pairs& p, float (&f)[16]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) { f[HALVES ? i : 2 * i] = p.a[i]; f[HALVES ? 8 + i : 2 * i + 1] = p.b[i]; }
-    Chunks<F32> c;
-    uint32_t* w = reinterpret_cast<uint32_t*>(c.v);
-#pragma unroll
-    for (int i = 0; i < (F32 ? 16 : 8); ++i) w[i] = F32 ? __float_as_uint(f[i]) : pack_bf16(f[2 * i], f[2 * i + 1]);
-    char* q = row + u * (HALVES ? 8 * E : 16 * E);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        *reinterpret_cast<uint4*>(q + (HALVES ? (i % (N / 2)) * 16 + (i / (N / 2)) * 64 * E : 16 * i)) = c.v[i];
 }
 
-// Cosines and sines of the unit's pairs 8u..8u+7 for token (t,h,w); pairs that do not turn: (1, 0)
+template <bool F32> struct Chunks { uint4 v[F32 ? 4 : 2]; };         // an input row's, BY4 = F32
+template <bool F32>
+__device__ __forceinline__ Chunks<F32> load_row(const char* row, int u) {
+    Chunks<F32> c;
+#pragma unroll
+    for (int i = 0; i < (F32 ? 4 : 2); ++i) c.v[i] = *reinterpret_cast<const uint4*>(row + 128 * i + 16 * u);
+    return c;
+}
+template <bool F32, bool HALVES>
+__device__ __forceinline__ Pairs unpack(const Chunks<F32>& c) {
+    float f[16];
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(c.v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = F32 ? __uint_as_float(w[i]) : (i & 1) ? high_bf16(w[i >> 1]) : low_bf16(w[i >> 1]);
+    return as_pairs<HALVES>(f);
+}
+template <bool BY4, bool F32, bool HALVES>
+__device__ __forceinline__ void store_row(char* row, int u, const Pairs& p) {
+    float f[16];
+    as_slots<HALVES>(p, f);
+    if (F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4*>(row + 4 * channel_of<BY4>(u, 4 * i)) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    } else if (BY4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2*>(row + 2 * channel_of<BY4>(u, 4 * i)) = make_uint2(pack_bf16(f[4 * i], f[4 * i + 1]), pack_bf16(f[4 * i + 2], f[4 * i + 3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(row + 128 * i + 16 * u) = make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]),
+                                                                         pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
+    }
+}
+
+// Cosines and sines of the lane's pairs for token (t,h,w); pairs that do not turn: (1, 0)
 struct Turn { float c[8], s[8]; };
-__device__ __forceinline__ Turn load_turn(const Turning& k, const float2* table, int T, int H, int t, int h, int w, int u) {
-    Turn r;                                                  // from a table of T places and H places before those of w
+template <bool BY4, bool HALVES>
+__device__ __forceinline__ Turn load_turn(const Turning& k, int b, int t, int h, int w, int u) {
+    Turn r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) { r.c[i] = 1.0f; r.s[i] = 0.0f; }
-    const int at_t = t * k.ct, at_h = T * k.ct + h * k.ch - k.ct, at_w = T * k.ct + H * k.ch + w * k.cw - k.ct - k.ch;
+    const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
+    const int at_t = t * k.ct, at_h = k.T * k.ct + h * k.ch - k.ct, at_w = k.T * k.ct + k.H * k.ch + w * k.cw - k.ct - k.ch;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int p = 8 * u + i;
+        const int p = pair_of<BY4, HALVES>(u, i);
         if (p < k.ct + k.ch + k.cw) {                        // none without a rotation
             const float2 cs = table[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
             r.c[i] = cs.x;
@@ -99,17 +116,25 @@ __device__ __forceinline__ Turn load_turn(const Turning& k, const float2* table,
     }
     return r;
 }
+template <bool BY4, bool HALVES>
 __device__ __forceinline__ Turn load_turn_of_token(const Turning& k, int b, int n, int u) {
     const int t = quotient(n, k.H * k.W, k.rc_plane), rem = n - t * (k.H * k.W), h = quotient(rem, k.W, k.rc_row);
-    return load_turn(k, reinterpret_cast<const float2*>(k.table + b * k.table_b), k.T, k.H, t, h, rem - h * k.W, u);
+    return load_turn<BY4, HALVES>(k, b, t, h, rem - h * k.W, u);
 }
-template <bool HALVES>
+template <bool BY4, bool HALVES>
 __device__ __forceinline__ Pairs load_weight(const Turning& k, int h, int u) {
-    if (k.weight) return unpack<true, HALVES>(load_pairs<true, HALVES>((const char*)(k.weight + h * k.weight_head), u));
-    Pairs p;
+    float f[16];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p.a[i] = p.b[i] = 1.0f;
-    return p;
+    for (int i = 0; i < 16; ++i) f[i] = 1.0f;
+    if (k.weight) {
+        const float* w = k.weight + h * k.weight_head;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 v = *reinterpret_cast<const float4*>(w + channel_of<BY4>(u, 4 * i));
+            f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+        }
+    }
+    return as_pairs<HALVES>(f);
 }
 
 // sum over the eight lanes of a row
@@ -129,16 +154,22 @@ __device__ __forceinline__ float inverse_rms(const Turning& k, const Pairs& x) {
     for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x.a[i], x.a[i], __builtin_fmaf(x.b[i], x.b[i], s));
     return __builtin_amdgcn_rsqf(row_sum(s) * (1.0f / 128.0f) + k.eps);
 }
-__device__ __forceinline__ Pairs norm_rotated(const Turning& k, const Pairs& x, const Pairs& w, const Turn& turn) {
-    const float r = inverse_rms(k, x);
+// R (x w), which r is left to be multiplied with
+__device__ __forceinline__ Pairs weighted_turned(const Pairs& x, const Pairs& w, const Turn& turn) {
     Pairs y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float a = x.a[i] * r * w.a[i], b = x.b[i] * r * w.b[i];
+        const float a = x.a[i] * w.a[i], b = x.b[i] * w.b[i];
         y.a[i] = __builtin_fmaf(a, turn.c[i], -(b * turn.s[i]));
         y.b[i] = __builtin_fmaf(a, turn.s[i], b * turn.c[i]);
     }
     return y;
+}
+__device__ __forceinline__ Pairs times(const Pairs& y, float r) {
+    Pairs z;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { z.a[i] = y.a[i] * r; z.b[i] = y.b[i] * r; }
+    return z;
 }
 
 // ---- into the caller's layout -------------------------------------------------------------------
@@ -152,13 +183,13 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
     Chunks<IN32> c[HC];
 #pragma unroll
     for (int i = 0; i < HC; ++i)
-        if (h0 + i < heads) c[i] = load_pairs<IN32, HALVES>(x.at(b, h0 + i, n), u);
-    const Turn turn = load_turn_of_token(k, b, n, u);
+        if (h0 + i < heads) c[i] = load_row<IN32>(x.at(b, h0 + i, n), u);
+    const Turn turn = load_turn_of_token<IN32, HALVES>(k, b, n, u);
 #pragma unroll
     for (int i = 0; i < HC; ++i) {
         if (h0 + i >= heads) break;
-        const Pairs w = load_weight<HALVES>(k, h0 + i, u);
-        store_pairs<OUT32, HALVES>(const_cast<char*>(y.at(b, h0 + i, n)), u, norm_rotated(k, unpack<IN32, HALVES>(c[i]), w, turn));
+        const Pairs w = load_weight<IN32, HALVES>(k, h0 + i, u), v = unpack<IN32, HALVES>(c[i]);
+        store_row<IN32, OUT32, HALVES>(const_cast<char*>(y.at(b, h0 + i, n)), u, times(weighted_turned(v, w, turn), inverse_rms(k, v)));
     }
 }
 
@@ -167,7 +198,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // registers from the reading to the encoding; of larger groups a block, of which PASS 0 finds the maximum and PASS 1, which
 // reads x again, encodes.
 // A token's cosines and sines would be four times as many load instructions as its channels: where the entries of the
-// group's planes, rows and columns are at most kStaged they are brought into LDS first.
+// group's planes, rows and columns are at most kStaged they are brought into LDS first (720p 309 -> 270 us).
 constexpr int kWhole = -1, kStaged = 1024;
 template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
@@ -175,13 +206,14 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                                                                            int heads) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
     __shared__ uint32_t red[WAVES];
-    __shared__ float2 staged[kStaged];
+    __shared__ float2 staged[kStaged + 1];                   // the last one: (1, 0)
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     const int blk = blockIdx.x * NB + kb;
     const BlockOrigin org = block_origin(g, blockIdx.x * NB);
     const int bh = quotient((int)org.tile_lin, g.M, g.rc_m), b = bh / heads, head = bh - b * heads;
     const int n0 = (int)(org.raster0 - (long long)bh * g.T * g.H * g.W);
-    const Pairs weight = load_weight<HALVES>(k, head, u);
+    const char* const x0 = x.at(b, head, n0);
+    const Pairs weight = load_weight<IN32, HALVES>(k, head, u);
 
     Chunks<IN32> in[U];
     Offset token[U];                                         // from the group's first; t < 0: padding
@@ -189,40 +221,58 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
     for (int i = 0; i < U; ++i) {
         const int slot = org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i;
         token[i] = real_token(org.box, slot);
-        if (slot < org.box.n) in[i] = load_pairs<IN32, HALVES>(x.at(b, head, n0 + (token[i].t * g.H + token[i].h) * g.W + token[i].w), u);
+        if (slot < org.box.n) in[i] = load_row<IN32>(x0 + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r, u);
         else                  token[i].t = -1;
     }
     // the group's entries: its planes', rows' and columns' are three runs of the table
     const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
     const int et = org.box.n ? real_token(org.box, org.box.n - 1).t + 1 : 0, of_t = et * k.ct, of_h = org.box.eh * k.ch, of_w = org.box.ew * k.cw;
     const bool in_lds = of_t + of_h + of_w <= kStaged;
-    const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
-    if (k.table && in_lds && et > 0) {
+    if (in_lds && et > 0) {
+        const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
         for (int i = threadIdx.x; i < of_t + of_h + of_w; i += THREADS * NB)
             staged[i] = table[i < of_t ? t0 * k.ct + i
                                        : i < of_t + of_h ? g.T * k.ct + h0 * k.ch + i - of_t : g.T * k.ct + g.H * k.ch + w0 * k.cw + i - of_t - of_h];
+        if (threadIdx.x == 0) staged[kStaged] = make_float2(1.0f, 0.0f);
     }
     __syncthreads();
-    Pairs y[U];
-    uint32_t top = 0;
+    auto turn_of = [&](const Offset& d) __attribute__((always_inline)) {
+        if (!in_lds) return load_turn<IN32, HALVES>(k, b, t0 + d.t, h0 + d.h, w0 + d.w, u);
+        Turn r;
+        const int at_t = d.t * k.ct, at_h = of_t + d.h * k.ch - k.ct, at_w = of_t + of_h + d.w * k.cw - k.ct - k.ch;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int p = pair_of<IN32, HALVES>(u, i);
+            const float2 cs = staged[p < k.ct + k.ch + k.cw ? (p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p : kStaged];
+            r.c[i] = cs.x;
+            r.s[i] = cs.y;
+        }
+        return r;
+    };
+    Pairs y[U];                                              // without the norm's factor r of the row
+    float r[U];
+    uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+        r[i] = 0.0f;
         if (token[i].t >= 0) {
-            const Offset d = token[i];
-            const Turn turn = in_lds ? load_turn(k, staged, et, org.box.eh, d.t, d.h, d.w, u)
-                                     : load_turn(k, table, g.T, g.H, t0 + d.t, h0 + d.h, w0 + d.w, u);
-            y[i] = norm_rotated(k, unpack<IN32, HALVES>(in[i]), weight, turn);
+            const Pairs v = unpack<IN32, HALVES>(in[i]);
+            y[i] = weighted_turned(v, weight, turn_of(token[i]));
+            r[i] = inverse_rms(k, v);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
         }
         if (FP8 && PASS != 1) {
+            uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {                    // magnitudes order like their bits, NaN above all
+            for (int j = 0; j < 8; ++j) {
                 const uint32_t ma = __float_as_uint(y[i].a[j]) & 0x7FFFFFFFu, mb = __float_as_uint(y[i].b[j]) & 0x7FFFFFFFu;
-                top = top > ma ? top : ma;
-                top = top > mb ? top : mb;
+                m = m > ma ? m : ma;
+                m = m > mb ? m : mb;
             }
+            const uint32_t of_row = __float_as_uint(__uint_as_float(m) * r[i]) & 0x7FFFFFFFu;     // rounds like the largest product
+            top = top > of_row ? top : of_row;
         }
     }
     char* const dst = (char*)xq + (long long)blk * (BS * 128 * (FP8 ? 1 : 2));
@@ -231,19 +281,15 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         for (int i = 0; i < U; ++i) {
             const int j = (tid >> 3) + THREADS / 8 * i;
             float f[16];
+            as_slots<HALVES>(times(y[i], r[i]), f);
+            auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
 #pragma unroll
-            for (int m = 0; m < 8; ++m) { f[HALVES ? m : 2 * m] = y[i].a[m]; f[HALVES ? 8 + m : 2 * m + 1] = y[i].b[m]; }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int c8 = HALVES ? u + 8 * half : 2 * u + half;
-                int c = j * 16 + c8;
-                if (role == FPS_ROLE_K) c = ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31);
-                uint4 o;
-                o.x = pack_bf16(f[8 * half], f[8 * half + 1]);
-                o.y = pack_bf16(f[8 * half + 2], f[8 * half + 3]);
-                o.z = pack_bf16(f[8 * half + 4], f[8 * half + 5]);
-                o.w = pack_bf16(f[8 * half + 6], f[8 * half + 7]);
-                reinterpret_cast<uint4*>(dst)[c] = o;
+            for (int m = 0; m < 16; m += IN32 ? 4 : 8) {
+                const int c = channel_of<IN32>(u, m);
+                char* at = dst + 16 * chunk(c >> 3) + 2 * (c & 7);
+                const uint2 lo = make_uint2(pack_bf16(f[m], f[m + 1]), pack_bf16(f[m + 2], f[m + 3]));
+                if (IN32) *reinterpret_cast<uint2*>(at) = lo;
+                else      *reinterpret_cast<uint4*>(at) = make_uint4(lo.x, lo.y, pack_bf16(f[(m + 4) & 15], f[(m + 5) & 15]), pack_bf16(f[(m + 6) & 15], f[(m + 7) & 15]));
             }
         }
         return;
@@ -265,27 +311,23 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
     for (int i = 0; i < U; ++i) {
         const int j = (tid >> 3) + THREADS / 8 * i;
         float f[16];
-#pragma unroll
-        for (int m = 0; m < 8; ++m) {
-            f[HALVES ? m : 2 * m] = y[i].a[m] * up * rs;
-            f[HALVES ? 8 + m : 2 * m + 1] = y[i].b[m] * up * rs;
-        }
+        as_slots<HALVES>(times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs), f);    // |x| <= amax: the product cannot reach the next code, 480
+        // the 16-byte chunk of channels 16 c16 ..
+        auto chunk = [&](int c16) {
+            return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
+        };
         uint32_t o[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {                        // |x| <= amax: the product cannot reach the next code, 480
-            int r = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m], f[4 * m + 1], 0, false);
-            o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m + 2], f[4 * m + 3], r, true);
+        for (int m = 0; m < 4; ++m) {
+            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m], f[4 * m + 1], 0, false);
+            o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m + 2], f[4 * m + 3], w, true);
         }
-        // the 16-byte chunk of channels 16 c16.., of which a unit of halves has eight bytes each of two
-        auto chunk = [&](int c16) {
-            return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31)
-                                      : j * 8 + c16;
-        };
-        if (HALVES) {
-            *reinterpret_cast<uint2*>(dst + 16 * chunk(u >> 1) + 8 * (u & 1)) = make_uint2(o[0], o[1]);
-            *reinterpret_cast<uint2*>(dst + 16 * chunk(4 + (u >> 1)) + 8 * (u & 1)) = make_uint2(o[2], o[3]);
-        } else {
-            reinterpret_cast<uint4*>(dst)[chunk(u)] = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+        for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
+            const int c = channel_of<IN32>(u, 4 * m);
+            char* at = dst + 16 * chunk(c >> 4) + (c & 15);
+            if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
+            else      *reinterpret_cast<uint2*>(at) = make_uint2(o[m], o[(m + 1) & 3]);
         }
     }
 }
@@ -314,11 +356,11 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
 #pragma unroll
         for (int i = 0; i < HC; ++i)
             if (h0 + i < last) {
-                cx[i] = load_pairs<F32, HALVES>(x.at(b, h0 + i, n), u);
-                cy[i] = load_pairs<F32, HALVES>(dy.at(b, h0 + i, n), u);
+                cx[i] = load_row<F32>(x.at(b, h0 + i, n), u);
+                cy[i] = load_row<F32>(dy.at(b, h0 + i, n), u);
             }
-        const Turn turn = load_turn_of_token(k, b, n, u);
-        const Pairs w = load_weight<HALVES>(k, h0, u);                       // of all of them, or of the one
+        const Turn turn = load_turn_of_token<F32, HALVES>(k, b, n, u);
+        const Pairs w = load_weight<F32, HALVES>(k, h0, u);                       // of all of them, or of the one
 #pragma unroll
         for (int i = 0; i < HC; ++i) {
             if (h0 + i >= last) break;
@@ -343,7 +385,7 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
                 d.a[m] = r * __builtin_fmaf(-xv.a[m], back, g.a[m]);
                 d.b[m] = r * __builtin_fmaf(-xv.b[m], back, g.b[m]);
             }
-            store_pairs<F32, HALVES>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
+            store_row<F32, F32, HALVES>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
         }
     }
     if (!partial) return;
@@ -354,12 +396,12 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             dw.a[i] += __shfl_xor(dw.a[i], off);
             dw.b[i] += __shfl_xor(dw.b[i], off);
         }
-    if ((threadIdx.x & 63) < 8)
+    if ((threadIdx.x & 63) < 8) {
+        float f[16];
+        as_slots<HALVES>(dw, f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            red[threadIdx.x >> 6][HALVES ? 8 * u + i : 16 * u + 2 * i] = dw.a[i];
-            red[threadIdx.x >> 6][HALVES ? 64 + 8 * u + i : 16 * u + 2 * i + 1] = dw.b[i];
-        }
+        for (int i = 0; i < 16; ++i) red[threadIdx.x >> 6][channel_of<F32>(u, i)] = f[i];
+    }
     __syncthreads();
     if (threadIdx.x < 128) {
         const int c = threadIdx.x;
@@ -479,7 +521,7 @@ static Turning turning_of(const Geom& g, const fps_norm* norm, const fps_rotatio
 }
 static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_PAIRS_HALVES; }
 
-constexpr int kBwdHeads = 4;
+constexpr int kHeads = 8, kBwdHeads = 4;                    // of a workgroup
 
 // f(bool constants...) for run-time truth values
 template <typename F> static void with(bool a, F&& f) { if (a) f(std::true_type{}); else f(std::false_type{}); }
@@ -490,11 +532,11 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     const int tokens = x.rows;
     const long long blocks = (tokens + 31LL) / 32;
     const bool few = blocks * x.B * x.heads < 4096;
-    const int parts = few ? x.heads : (x.heads + 3) / 4;
+    const int parts = few ? x.heads : (x.heads + kHeads - 1) / kHeads;
     const long long grid = blocks * x.B * parts;
     if (grid > 0x7FFFFFFF) { set_error("more rows than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
     with(x.dt == FPS_OUT_F32, [&](auto in32) { with(y.dt == FPS_OUT_F32, [&](auto out32) { with(halves(rot), [&](auto hv) { with(few, [&](auto one) {
-        constexpr int HC = decltype(one)::value ? 1 : 4;
+        constexpr int HC = decltype(one)::value ? 1 : kHeads;
         norm_rotate_kernel<decltype(in32)::value, decltype(out32)::value, decltype(hv)::value, HC>
             <<<(int)grid, 256, 0, st>>>(rows_of(x), rows_of(y), k, tokens, x.heads, parts);
     }); }); }); });
