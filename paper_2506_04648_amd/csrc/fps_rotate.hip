@@ -49,15 +49,14 @@ template <bool BY4> __device__ __forceinline__ int channel_of(int u, int s) { re
 template <bool BY4, bool HALVES> __device__ __forceinline__ int pair_of(int u, int i) {
     return HALVES ? channel_of<BY4>(u, i) : channel_of<BY4>(u, 2 * i) >> 1;
 }
-template <bool HALVES> __device__ __forceinline__ Pairs as_pairs(const float (&f)[16]) {
+template <bool HALVES> __device__ __forceinline__ float slot_of(const Pairs& p, int s) {
+    return HALVES ? (s < 8 ? p.a[s & 7] : p.b[s & 7]) : (s & 1) ? p.b[s >> 1] : p.a[s >> 1];
+}
+template <bool HALVES, typename F> __device__ __forceinline__ Pairs pairs_of(F&& slot) {
     Pairs p;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { p.a[i] = f[HALVES ? i : 2 * i]; p.b[i] = f[HALVES ? 8 + i : 2 * i + 1]; }
+    for (int i = 0; i < 8; ++i) { p.a[i] = slot(HALVES ? i : 2 * i); p.b[i] = slot(HALVES ? 8 + i : 2 * i + 1); }
     return p;
-}
-template <bool HALVES> __device__ __forceinline__ void as_slots(const Pairs& p, float (&f)[16]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { f[HALVES ? i : 2 * i] = p.a[i]; f[HALVES ? 8 + i : 2 * i + 1] = p.b[i]; }
 }
 
 template <bool F32> struct Chunks { uint4 v[F32 ? 4 : 2]; };         // an input row's, BY4 = F32
@@ -70,71 +69,65 @@ __device__ __forceinline__ Chunks<F32> load_row(const char* row, int u) {
 }
 template <bool F32, bool HALVES>
 __device__ __forceinline__ Pairs unpack(const Chunks<F32>& c) {
-    float f[16];
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(c.v);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = F32 ? __uint_as_float(w[i]) : (i & 1) ? high_bf16(w[i >> 1]) : low_bf16(w[i >> 1]);
-    return as_pairs<HALVES>(f);
+    return pairs_of<HALVES>([&](int s) __attribute__((always_inline)) {
+        const int i = F32 ? s : s >> 1;
+        const uint4 v = c.v[i >> 2];
+        const uint32_t w = (i & 3) == 0 ? v.x : (i & 3) == 1 ? v.y : (i & 3) == 2 ? v.z : v.w;
+        return F32 ? __uint_as_float(w) : (s & 1) ? high_bf16(w) : low_bf16(w);
+    });
 }
 template <bool BY4, bool F32, bool HALVES>
 __device__ __forceinline__ void store_row(char* row, int u, const Pairs& p) {
-    float f[16];
-    as_slots<HALVES>(p, f);
+    auto f = [&](int s) __attribute__((always_inline)) { return slot_of<HALVES>(p, s); };
+    auto two = [&](int s) __attribute__((always_inline)) { return pack_bf16(f(s), f(s + 1)); };
     if (F32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<float4*>(row + 4 * channel_of<BY4>(u, 4 * i)) = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(row + 4 * channel_of<BY4>(u, i)) = make_float4(f(i), f(i + 1), f(i + 2), f(i + 3));
     } else if (BY4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint2*>(row + 2 * channel_of<BY4>(u, 4 * i)) = make_uint2(pack_bf16(f[4 * i], f[4 * i + 1]), pack_bf16(f[4 * i + 2], f[4 * i + 3]));
+        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint2*>(row + 2 * channel_of<BY4>(u, i)) = make_uint2(two(i), two(i + 2));
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4*>(row + 128 * i + 16 * u) = make_uint4(pack_bf16(f[8 * i], f[8 * i + 1]), pack_bf16(f[8 * i + 2], f[8 * i + 3]),
-                                                                         pack_bf16(f[8 * i + 4], f[8 * i + 5]), pack_bf16(f[8 * i + 6], f[8 * i + 7]));
+        for (int i = 0; i < 16; i += 8) *reinterpret_cast<uint4*>(row + 2 * channel_of<BY4>(u, i)) = make_uint4(two(i), two(i + 2), two(i + 4), two(i + 6));
     }
 }
 
 // Cosines and sines of the lane's pairs for token (t,h,w); pairs that do not turn: (1, 0)
 struct Turn { float c[8], s[8]; };
 template <bool BY4, bool HALVES>
-__device__ __forceinline__ Turn load_turn(const Turning& k, int b, int t, int h, int w, int u) {
+__device__ __forceinline__ Turn load_turn(const Turning& k, int b, int n, int u) {
     Turn r;
+    if (!k.table) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { r.c[i] = 1.0f; r.s[i] = 0.0f; }
+        for (int i = 0; i < 8; ++i) { r.c[i] = 1.0f; r.s[i] = 0.0f; }
+        return r;
+    }
+    const int t = quotient(n, k.H * k.W, k.rc_plane), rem = n - t * (k.H * k.W), h = quotient(rem, k.W, k.rc_row), w = rem - h * k.W;
     const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
     const int at_t = t * k.ct, at_h = k.T * k.ct + h * k.ch - k.ct, at_w = k.T * k.ct + k.H * k.ch + w * k.cw - k.ct - k.ch;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {                            // without a branch: those that stay read the first entry
         const int p = pair_of<BY4, HALVES>(u, i);
-        if (p < k.ct + k.ch + k.cw) {                        // none without a rotation
-            const float2 cs = table[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
-            r.c[i] = cs.x;
-            r.s[i] = cs.y;
-        }
+        const bool turns = p < k.ct + k.ch + k.cw;
+        const float2 cs = table[turns ? (p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p : 0];
+        r.c[i] = turns ? cs.x : 1.0f;
+        r.s[i] = turns ? cs.y : 0.0f;
     }
     return r;
 }
 template <bool BY4, bool HALVES>
-__device__ __forceinline__ Turn load_turn_of_token(const Turning& k, int b, int n, int u) {
-    const int t = quotient(n, k.H * k.W, k.rc_plane), rem = n - t * (k.H * k.W), h = quotient(rem, k.W, k.rc_row);
-    return load_turn<BY4, HALVES>(k, b, t, h, rem - h * k.W, u);
-}
-template <bool BY4, bool HALVES>
 __device__ __forceinline__ Pairs load_weight(const Turning& k, int h, int u) {
-    float f[16];
+    float4 v[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = 1.0f;
+    for (int i = 0; i < 4; ++i) v[i] = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
     if (k.weight) {
-        const float* w = k.weight + h * k.weight_head;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4*>(w + channel_of<BY4>(u, 4 * i));
-            f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
-        }
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(k.weight + h * k.weight_head + channel_of<BY4>(u, 4 * i));
     }
-    return as_pairs<HALVES>(f);
+    return pairs_of<HALVES>([&](int s) __attribute__((always_inline)) {
+        const float4 f = v[s >> 2];
+        return (s & 3) == 0 ? f.x : (s & 3) == 1 ? f.y : (s & 3) == 2 ? f.z : f.w;
+    });
 }
 
 // sum over the eight lanes of a row
@@ -184,7 +177,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 #pragma unroll
     for (int i = 0; i < HC; ++i)
         if (h0 + i < heads) c[i] = load_row<IN32>(x.at(b, h0 + i, n), u);
-    const Turn turn = load_turn_of_token<IN32, HALVES>(k, b, n, u);
+    const Turn turn = load_turn<IN32, HALVES>(k, b, n, u);
 #pragma unroll
     for (int i = 0; i < HC; ++i) {
         if (h0 + i >= heads) break;
@@ -198,15 +191,16 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // registers from the reading to the encoding; of larger groups a block, of which PASS 0 finds the maximum and PASS 1, which
 // reads x again, encodes.
 // A token's cosines and sines would be four times as many load instructions as its channels: where the entries of the
-// group's planes, rows and columns are at most kStaged they are brought into LDS first (720p 309 -> 270 us).
+// group's planes, rows and columns, those of the columns filled up to 64 pairs, are at most kStaged they are brought into LDS
+// first (STAGED; 720p 309 -> 270 us).
 constexpr int kWhole = -1, kStaged = 1024;
-template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS>
+template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
                                                                            float* __restrict__ scales, int role, Geom g,
                                                                            int heads) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
     __shared__ uint32_t red[WAVES];
-    __shared__ float2 staged[kStaged + 1];                   // the last one: (1, 0)
+    __shared__ float2 staged[STAGED ? kStaged : 1];
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     const int blk = blockIdx.x * NB + kb;
     const BlockOrigin org = block_origin(g, blockIdx.x * NB);
@@ -224,26 +218,30 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         if (slot < org.box.n) in[i] = load_row<IN32>(x0 + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r, u);
         else                  token[i].t = -1;
     }
-    // the group's entries: its planes', rows' and columns' are three runs of the table
+    // the group's entries: its planes' and rows' are runs of the table, its columns' each a run and as many (1, 0) as there are pairs left
     const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
-    const int et = org.box.n ? real_token(org.box, org.box.n - 1).t + 1 : 0, of_t = et * k.ct, of_h = org.box.eh * k.ch, of_w = org.box.ew * k.cw;
-    const bool in_lds = of_t + of_h + of_w <= kStaged;
-    if (in_lds && et > 0) {
+    const int et = org.box.n ? real_token(org.box, org.box.n - 1).t + 1 : 0, rest = 64 - k.ct - k.ch;
+    const int of_t = et * k.ct, of_h = org.box.eh * k.ch, of_w = org.box.ew * rest;
+    if (STAGED && et > 0) {
         const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
-        for (int i = threadIdx.x; i < of_t + of_h + of_w; i += THREADS * NB)
-            staged[i] = table[i < of_t ? t0 * k.ct + i
-                                       : i < of_t + of_h ? g.T * k.ct + h0 * k.ch + i - of_t : g.T * k.ct + g.H * k.ch + w0 * k.cw + i - of_t - of_h];
-        if (threadIdx.x == 0) staged[kStaged] = make_float2(1.0f, 0.0f);
+        for (int i = threadIdx.x; i < of_t + of_h + of_w; i += THREADS * NB) {
+            int from = i < of_t ? t0 * k.ct + i : g.T * k.ct + h0 * k.ch + i - of_t;
+            if (i >= of_t + of_h) {
+                const int in_w = i - of_t - of_h, row = divide_small(in_w, rest), p = in_w - row * rest;
+                from = p < k.cw ? g.T * k.ct + g.H * k.ch + (w0 + row) * k.cw + p : -1;
+            }
+            staged[i] = from >= 0 ? table[from] : make_float2(1.0f, 0.0f);
+        }
     }
-    __syncthreads();
+    if (STAGED) __syncthreads();
     auto turn_of = [&](const Offset& d) __attribute__((always_inline)) {
-        if (!in_lds) return load_turn<IN32, HALVES>(k, b, t0 + d.t, h0 + d.h, w0 + d.w, u);
+        if (!STAGED) return load_turn<IN32, HALVES>(k, b, n0 + (d.t * g.H + d.h) * g.W + d.w, u);
         Turn r;
-        const int at_t = d.t * k.ct, at_h = of_t + d.h * k.ch - k.ct, at_w = of_t + of_h + d.w * k.cw - k.ct - k.ch;
+        const int at_t = d.t * k.ct, at_h = of_t + d.h * k.ch - k.ct, at_w = of_t + of_h + d.w * rest - k.ct - k.ch;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int p = pair_of<IN32, HALVES>(u, i);
-            const float2 cs = staged[p < k.ct + k.ch + k.cw ? (p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p : kStaged];
+            const float2 cs = staged[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
             r.c[i] = cs.x;
             r.s[i] = cs.y;
         }
@@ -280,16 +278,15 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int j = (tid >> 3) + THREADS / 8 * i;
-            float f[16];
-            as_slots<HALVES>(times(y[i], r[i]), f);
+            const Pairs z = times(y[i], r[i]);
+            auto two = [&](int s) __attribute__((always_inline)) { return pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)); };
             auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
 #pragma unroll
             for (int m = 0; m < 16; m += IN32 ? 4 : 8) {
                 const int c = channel_of<IN32>(u, m);
                 char* at = dst + 16 * chunk(c >> 3) + 2 * (c & 7);
-                const uint2 lo = make_uint2(pack_bf16(f[m], f[m + 1]), pack_bf16(f[m + 2], f[m + 3]));
-                if (IN32) *reinterpret_cast<uint2*>(at) = lo;
-                else      *reinterpret_cast<uint4*>(at) = make_uint4(lo.x, lo.y, pack_bf16(f[(m + 4) & 15], f[(m + 5) & 15]), pack_bf16(f[(m + 6) & 15], f[(m + 7) & 15]));
+                if (IN32) *reinterpret_cast<uint2*>(at) = make_uint2(two(m), two(m + 2));
+                else      *reinterpret_cast<uint4*>(at) = make_uint4(two(m), two(m + 2), two(m + 4), two(m + 6));
             }
         }
         return;
@@ -310,8 +307,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int j = (tid >> 3) + THREADS / 8 * i;
-        float f[16];
-        as_slots<HALVES>(times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs), f);    // |x| <= amax: the product cannot reach the next code, 480
+        const Pairs z = times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs);         // |x| <= amax: the product cannot reach the next code, 480
         // the 16-byte chunk of channels 16 c16 ..
         auto chunk = [&](int c16) {
             return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
@@ -319,8 +315,8 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         uint32_t o[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m], f[4 * m + 1], 0, false);
-            o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * m + 2], f[4 * m + 3], w, true);
+            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
+            o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
         }
 #pragma unroll
         for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
@@ -359,7 +355,7 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
                 cx[i] = load_row<F32>(x.at(b, h0 + i, n), u);
                 cy[i] = load_row<F32>(dy.at(b, h0 + i, n), u);
             }
-        const Turn turn = load_turn_of_token<F32, HALVES>(k, b, n, u);
+        const Turn turn = load_turn<F32, HALVES>(k, b, n, u);
         const Pairs w = load_weight<F32, HALVES>(k, h0, u);                       // of all of them, or of the one
 #pragma unroll
         for (int i = 0; i < HC; ++i) {
@@ -397,10 +393,8 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             dw.b[i] += __shfl_xor(dw.b[i], off);
         }
     if ((threadIdx.x & 63) < 8) {
-        float f[16];
-        as_slots<HALVES>(dw, f);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) red[threadIdx.x >> 6][channel_of<F32>(u, i)] = f[i];
+        for (int i = 0; i < 16; ++i) red[threadIdx.x >> 6][channel_of<F32>(u, i)] = slot_of<HALVES>(dw, i);
     }
     __syncthreads();
     if (threadIdx.x < 128) {
@@ -544,26 +538,26 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate launch");
 }
 
-template <int BS, bool IN32, bool HALVES>
+template <int BS, bool IN32, bool HALVES, bool STAGED>
 static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                            hipStream_t st) {
     constexpr int TH = BS == 128 ? 256 : 128;
     const int blocks = g.BH * g.M * g.KB, groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
         return;
     }
     auto whole = [&](auto nb) {
         constexpr int NB = decltype(nb)::value;
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, NB, kWhole><<<groups, TH * NB, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, NB, kWhole, STAGED><<<groups, TH * NB, 0, st>>>(x, k, xq, scales, role, g, heads);
     };
     if (g.KBS == 1)      whole(Count<1>{});
     else if (g.KBS == 2) whole(Count<2>{});
     else if (g.KBS == 3) whole(Count<3>{});
     else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
         amax_to_scale_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
 }
@@ -571,9 +565,10 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
 int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm* norm, const fps_rotation* rot, int role,
                                int prec, void* xq, float* scales, hipStream_t st) {
     const Turning k = turning_of(g, norm, rot);
-    with(g.BS == 128, [&](auto big) { with(x.dt == FPS_OUT_F32, [&](auto in32) { with(halves(rot), [&](auto hv) {
-        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value>(g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
-    }); }); });
+    const bool staged = (long long)g.Qt * k.ct + (long long)g.Qh * k.ch + (long long)g.Qw * (64 - k.ct - k.ch) <= kStaged;
+    with(g.BS == 128, [&](auto big) { with(x.dt == FPS_OUT_F32, [&](auto in32) { with(halves(rot), [&](auto hv) { with(staged, [&](auto sg) {
+        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value>(g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
+    }); }); }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");
 }
