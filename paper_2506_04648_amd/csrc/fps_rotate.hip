@@ -140,6 +140,12 @@ __device__ __forceinline__ float row_sum(float x) {
     add(Count<0x141>{});           // the other four of eight
     return x;
 }
+// the largest of m and two magnitudes; NaN if one of them is
+__device__ __forceinline__ float max_magnitude(float m, float a, float b) {
+    float r;
+    asm("v_maximum3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(m), "v"(a), "v"(b));
+    return r;
+}
 __device__ __forceinline__ float inverse_rms(const Turning& k, const Pairs& x) {
     if (!k.norm) return 1.0f;
     float s = 0.0f;
@@ -190,9 +196,10 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // As quantize_tiles_kernel (and pack_bf16_kernel): a workgroup is one scale group of up to three blocks, held in
 // registers from the reading to the encoding; of larger groups a block, of which PASS 0 finds the maximum and PASS 1, which
 // reads x again, encodes.
-// A token's cosines and sines would be four times as many load instructions as its channels: where the entries of the
-// group's planes, rows and columns, those of the columns filled up to 64 pairs, are at most kStaged they are brought into LDS
-// first (STAGED; 720p 309 -> 270 us).
+// A token's cosines and sines would be four times as many load instructions as its channels, and all the arithmetic is as long as the
+// memory takes: where the entries of the group's planes, rows and columns, those of the columns filled up to 64 pairs, are at most
+// kStaged (STAGED) they are brought into LDS first, for FP8 multiplied by the pair's weights: (x, y) -> (x A - y B, x C + y D).  (BF16
+// operands are, bit for bit, the packed bf16 tensor, and take the products in its order.)
 constexpr int kWhole = -1, kStaged = 1024;
 template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
@@ -200,76 +207,82 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                                                                            int heads) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
     __shared__ uint32_t red[WAVES];
-    __shared__ float2 staged[STAGED ? kStaged : 1];
+    __shared__ __attribute__((aligned(16))) float4 staged[STAGED ? kStaged : 1];
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
+    load_arguments<6>();
     const int blk = blockIdx.x * NB + kb;
     const BlockOrigin org = block_origin(g, blockIdx.x * NB);
     const int bh = quotient((int)org.tile_lin, g.M, g.rc_m), b = bh / heads, head = bh - b * heads;
     const int n0 = (int)(org.raster0 - (long long)bh * g.T * g.H * g.W);
     const char* const x0 = x.at(b, head, n0);
-    const Pairs weight = load_weight<IN32, HALVES>(k, head, u);
 
     Chunks<IN32> in[U];
-    Offset token[U];                                         // from the group's first; t < 0: padding
+    Offset token[U];                                         // from the group's first; padding is zeros at the place of the last token
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int slot = org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i;
-        token[i] = real_token(org.box, slot);
+        token[i] = real_token(org.box, slot < org.box.n ? slot : org.box.n > 0 ? org.box.n - 1 : 0);
+        in[i] = Chunks<IN32>{};
         if (slot < org.box.n) in[i] = load_row<IN32>(x0 + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r, u);
-        else                  token[i].t = -1;
     }
     // the group's entries: its planes' and rows' are runs of the table, its columns' each a run and as many (1, 0) as there are pairs left
     const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
     const int et = org.box.n ? real_token(org.box, org.box.n - 1).t + 1 : 0, rest = 64 - k.ct - k.ch;
     const int of_t = et * k.ct, of_h = org.box.eh * k.ch, of_w = org.box.ew * rest;
-    if (STAGED && et > 0) {
+    if (STAGED) {                                            // a thread one pair's entries of every fourth (eighth, ..) place
+        const int p = threadIdx.x & 63, axis = p < k.ct ? 0 : p < k.ct + k.ch ? 1 : 2;
+        const int a = HALVES ? p : 2 * p, c = axis == 0 ? k.ct : axis == 1 ? k.ch : rest, q = axis == 0 ? p : axis == 1 ? p - k.ct : p - k.ct - k.ch;
+        const int places = org.box.n == 0 ? 1 : axis == 0 ? et : axis == 1 ? org.box.eh : org.box.ew;
+        const int from = axis == 0 ? t0 * k.ct : axis == 1 ? g.T * k.ct + h0 * k.ch : g.T * k.ct + g.H * k.ch + w0 * k.cw;
+        const int step = axis == 2 ? k.cw : c, to = axis == 0 ? 0 : axis == 1 ? of_t : of_t + of_h;
+        const bool turns = org.box.n > 0 && (axis < 2 || q < k.cw);
         const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
-        for (int i = threadIdx.x; i < of_t + of_h + of_w; i += THREADS * NB) {
-            int from = i < of_t ? t0 * k.ct + i : g.T * k.ct + h0 * k.ch + i - of_t;
-            if (i >= of_t + of_h) {
-                const int in_w = i - of_t - of_h, row = divide_small(in_w, rest), p = in_w - row * rest;
-                from = p < k.cw ? g.T * k.ct + g.H * k.ch + (w0 + row) * k.cw + p : -1;
+        const float* w = k.weight + head * k.weight_head + a;
+        const float wa = k.weight ? w[0] : 1.0f, wb = k.weight ? w[HALVES ? 64 : 1] : 1.0f;
+        constexpr int R = THREADS * NB / 64, L = 4;          // places at a time, loads at a time
+        for (int first = threadIdx.x >> 6; first < places; first += L * R) {
+            float2 cs[L];
+#pragma unroll
+            for (int l = 0; l < L; ++l) {
+                cs[l] = make_float2(1.0f, 0.0f);
+                if (turns) cs[l] = table[from + min_of(first + l * R, places - 1) * step + q];
             }
-            staged[i] = from >= 0 ? table[from] : make_float2(1.0f, 0.0f);
+#pragma unroll
+            for (int l = 0; l < L; ++l)
+                if (first + l * R < places)
+                    staged[to + (first + l * R) * c + q] = FP8 ? make_float4(wa * cs[l].x, wb * cs[l].y, wa * cs[l].y, wb * cs[l].x)
+                                                               : make_float4(cs[l].x, cs[l].y, wa, wb);
         }
     }
     if (STAGED) __syncthreads();
-    auto turn_of = [&](const Offset& d) __attribute__((always_inline)) {
-        if (!STAGED) return load_turn<IN32, HALVES>(k, b, n0 + (d.t * g.H + d.h) * g.W + d.w, u);
-        Turn r;
+    auto turned = [&](const Pairs& v, const Offset& d) __attribute__((always_inline)) {
+        if (!STAGED) return weighted_turned(v, load_weight<IN32, HALVES>(k, head, u),
+                                            load_turn<IN32, HALVES>(k, b, min_of(n0 + (d.t * g.H + d.h) * g.W + d.w, g.T * g.H * g.W - 1), u));
+        Pairs y;
         const int at_t = d.t * k.ct, at_h = of_t + d.h * k.ch - k.ct, at_w = of_t + of_h + d.w * rest - k.ct - k.ch;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int p = pair_of<IN32, HALVES>(u, i);
-            const float2 cs = staged[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
-            r.c[i] = cs.x;
-            r.s[i] = cs.y;
+            const float4 f = staged[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
+            const float a = FP8 ? v.a[i] : v.a[i] * f.z, b = FP8 ? v.b[i] : v.b[i] * f.w;
+            y.a[i] = __builtin_fmaf(a, f.x, -(b * f.y));
+            y.b[i] = __builtin_fmaf(a, FP8 ? f.z : f.y, b * (FP8 ? f.w : f.x));
         }
-        return r;
+        return y;
     };
     Pairs y[U];                                              // without the norm's factor r of the row
     float r[U];
     uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        r[i] = 0.0f;
-        if (token[i].t >= 0) {
-            const Pairs v = unpack<IN32, HALVES>(in[i]);
-            y[i] = weighted_turned(v, weight, turn_of(token[i]));
-            r[i] = inverse_rms(k, v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
-        }
+        const Pairs v = unpack<IN32, HALVES>(in[i]);
+        y[i] = turned(v, token[i]);
+        r[i] = inverse_rms(k, v);
         if (FP8 && PASS != 1) {
-            uint32_t m = 0;
+            float m = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t ma = __float_as_uint(y[i].a[j]) & 0x7FFFFFFFu, mb = __float_as_uint(y[i].b[j]) & 0x7FFFFFFFu;
-                m = m > ma ? m : ma;
-                m = m > mb ? m : mb;
-            }
-            const uint32_t of_row = __float_as_uint(__uint_as_float(m) * r[i]) & 0x7FFFFFFFu;     // rounds like the largest product
+            for (int j = 0; j < 8; ++j) m = max_magnitude(m, y[i].a[j], y[i].b[j]);
+            const uint32_t of_row = __float_as_uint(m * r[i]) & 0x7FFFFFFFu;                        // rounds like the largest product
             top = top > of_row ? top : of_row;
         }
     }
@@ -279,7 +292,8 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         for (int i = 0; i < U; ++i) {
             const int j = (tid >> 3) + THREADS / 8 * i;
             const Pairs z = times(y[i], r[i]);
-            auto two = [&](int s) __attribute__((always_inline)) { return pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)); };
+            const bool real = org.slot0 + kb * BS + j < org.box.n;               // padding is 0, not -0
+            auto two = [&](int s) __attribute__((always_inline)) { return real ? pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)) : 0u; };
             auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
 #pragma unroll
             for (int m = 0; m < 16; m += IN32 ? 4 : 8) {
@@ -317,6 +331,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         for (int m = 0; m < 4; ++m) {
             const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
             o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
+            o[m] = org.slot0 + kb * BS + j < org.box.n ? o[m] : 0u;              // padding is 0, not -0
         }
 #pragma unroll
         for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
@@ -541,15 +556,17 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
 template <int BS, bool IN32, bool HALVES, bool STAGED>
 static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                            hipStream_t st) {
-    constexpr int TH = BS == 128 ? 256 : 128;
+    // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
+    // be more threads than a workgroup may have
+    constexpr int TH = BS == 128 ? 512 : 128;
     const int blocks = g.BH * g.M * g.KB, groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
         return;
     }
     auto whole = [&](auto nb) {
-        constexpr int NB = decltype(nb)::value;
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, NB, kWhole, STAGED><<<groups, TH * NB, 0, st>>>(x, k, xq, scales, role, g, heads);
+        constexpr int NB = decltype(nb)::value, T = TH * NB > 1024 ? TH / 2 : TH;
+        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED><<<groups, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads);
     };
     if (g.KBS == 1)      whole(Count<1>{});
     else if (g.KBS == 2) whole(Count<2>{});
