@@ -44,7 +44,8 @@ struct Turning {
 // channel 64 (s / 8) + 8u + s % 8, or, BY4 (fp32 input), 32 (s / 4) + 4u + s % 4.  Pair i of 8: slots 2i and 2i + 1, or, halves,
 // i and i + 8.  (Sixteen channels in a row to a lane, every load half of each line: 720p 350 us instead of 320, the gradient of
 // 480p 70 instead of 61.)
-struct Pairs { float a[8], b[8]; };
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+struct Pairs { f32x8 a, b; };                                // vectors: arrays end up in LDS where the compiler loses track of an index
 template <bool BY4> __device__ __forceinline__ int channel_of(int u, int s) { return BY4 ? 32 * (s >> 2) + 4 * u + (s & 3) : 64 * (s >> 3) + 8 * u + (s & 7); }
 template <bool BY4, bool HALVES> __device__ __forceinline__ int pair_of(int u, int i) {
     return HALVES ? channel_of<BY4>(u, i) : channel_of<BY4>(u, 2 * i) >> 1;
@@ -59,41 +60,52 @@ template <bool HALVES, typename F> __device__ __forceinline__ Pairs pairs_of(F&&
     return p;
 }
 
-template <bool F32> struct Chunks { uint4 v[F32 ? 4 : 2]; };         // an input row's, BY4 = F32
+// an input row's 16 channels, BY4 = F32
+template <bool F32> struct Chunks { uint32_t __attribute__((ext_vector_type(F32 ? 16 : 8))) w; };
 template <bool F32>
 __device__ __forceinline__ Chunks<F32> load_row(const char* row, int u) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     Chunks<F32> c;
 #pragma unroll
-    for (int i = 0; i < (F32 ? 4 : 2); ++i) c.v[i] = *reinterpret_cast<const uint4*>(row + 128 * i + 16 * u);
+    for (int i = 0; i < (F32 ? 4 : 2); ++i) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(row + 128 * i + 16 * u);
+        c.w[4 * i] = v.x; c.w[4 * i + 1] = v.y; c.w[4 * i + 2] = v.z; c.w[4 * i + 3] = v.w;
+    }
     return c;
 }
 template <bool F32, bool HALVES>
 __device__ __forceinline__ Pairs unpack(const Chunks<F32>& c) {
     return pairs_of<HALVES>([&](int s) __attribute__((always_inline)) {
-        const int i = F32 ? s : s >> 1;
-        const uint4 v = c.v[i >> 2];
-        const uint32_t w = (i & 3) == 0 ? v.x : (i & 3) == 1 ? v.y : (i & 3) == 2 ? v.z : v.w;
-        return F32 ? __uint_as_float(w) : (s & 1) ? high_bf16(w) : low_bf16(w);
+        if (F32) return __uint_as_float(c.w[s & (F32 ? 15 : 7)]);
+        return (s & 1) ? high_bf16(c.w[s >> 1]) : low_bf16(c.w[s >> 1]);
     });
 }
-template <bool BY4, bool F32, bool HALVES>
+// PAST: what is stored does not stay in the caches
+template <bool PAST>
+__device__ __forceinline__ void store_16(char* at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    if (PAST) __builtin_nontemporal_store(u32x4{x, y, z, w}, reinterpret_cast<u32x4*>(at));
+    else      *reinterpret_cast<u32x4*>(at) = u32x4{x, y, z, w};
+}
+template <bool BY4, bool F32, bool HALVES, bool PAST>
 __device__ __forceinline__ void store_row(char* row, int u, const Pairs& p) {
     auto f = [&](int s) __attribute__((always_inline)) { return slot_of<HALVES>(p, s); };
     auto two = [&](int s) __attribute__((always_inline)) { return pack_bf16(f(s), f(s + 1)); };
     if (F32) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(row + 4 * channel_of<BY4>(u, i)) = make_float4(f(i), f(i + 1), f(i + 2), f(i + 3));
+        for (int i = 0; i < 16; i += 4)
+            store_16<PAST>(row + 4 * channel_of<BY4>(u, i), __float_as_uint(f(i)), __float_as_uint(f(i + 1)), __float_as_uint(f(i + 2)), __float_as_uint(f(i + 3)));
     } else if (BY4) {
 #pragma unroll
         for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint2*>(row + 2 * channel_of<BY4>(u, i)) = make_uint2(two(i), two(i + 2));
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; i += 8) *reinterpret_cast<uint4*>(row + 2 * channel_of<BY4>(u, i)) = make_uint4(two(i), two(i + 2), two(i + 4), two(i + 6));
+        for (int i = 0; i < 16; i += 8) store_16<PAST>(row + 2 * channel_of<BY4>(u, i), two(i), two(i + 2), two(i + 4), two(i + 6));
     }
 }
 
 // Cosines and sines of the lane's pairs for token (t,h,w); pairs that do not turn: (1, 0)
-struct Turn { float c[8], s[8]; };
+struct Turn { f32x8 c, s; };
 template <bool BY4, bool HALVES>
 __device__ __forceinline__ Turn load_turn(const Turning& k, int b, int n, int u) {
     Turn r;
@@ -117,17 +129,20 @@ __device__ __forceinline__ Turn load_turn(const Turning& k, int b, int n, int u)
 }
 template <bool BY4, bool HALVES>
 __device__ __forceinline__ Pairs load_weight(const Turning& k, int h, int u) {
-    float4 v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    f32x8 lo = 1.0f, hi = 1.0f;
     if (k.weight) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float4*>(k.weight + h * k.weight_head + channel_of<BY4>(u, 4 * i));
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(k.weight + h * k.weight_head + channel_of<BY4>(u, 4 * i));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i < 2) lo[4 * i + j] = v[j];
+                else       hi[4 * (i & 1) + j] = v[j];
+            }
+        }
     }
-    return pairs_of<HALVES>([&](int s) __attribute__((always_inline)) {
-        const float4 f = v[s >> 2];
-        return (s & 3) == 0 ? f.x : (s & 3) == 1 ? f.y : (s & 3) == 2 ? f.z : f.w;
-    });
+    return pairs_of<HALVES>([&](int s) __attribute__((always_inline)) { return s < 8 ? lo[s & 7] : hi[s & 7]; });
 }
 
 // sum over the eight lanes of a row
@@ -173,7 +188,7 @@ __device__ __forceinline__ Pairs times(const Pairs& y, float r) {
 
 // ---- into the caller's layout -------------------------------------------------------------------
 // A wave takes eight tokens; each of its rows' cosines and sines are read once for HC heads.
-template <bool IN32, bool OUT32, bool HALVES, int HC>
+template <bool IN32, bool OUT32, bool HALVES, int HC, bool PAST>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turning k, int tokens, int heads, int parts) {
     const int blocks = (int)((tokens + 31u) >> 5), bp = blockIdx.x / blocks;        // tokens fastest
     const int u = threadIdx.x & 7, n = (blockIdx.x - bp * blocks) * 32 + (threadIdx.x >> 3);
@@ -188,7 +203,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
     for (int i = 0; i < HC; ++i) {
         if (h0 + i >= heads) break;
         const Pairs w = load_weight<IN32, HALVES>(k, h0 + i, u), v = unpack<IN32, HALVES>(c[i]);
-        store_row<IN32, OUT32, HALVES>(const_cast<char*>(y.at(b, h0 + i, n)), u, times(weighted_turned(v, w, turn), inverse_rms(k, v)));
+        store_row<IN32, OUT32, HALVES, PAST>(const_cast<char*>(y.at(b, h0 + i, n)), u, times(weighted_turned(v, w, turn), inverse_rms(k, v)));
     }
 }
 
@@ -222,7 +237,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
     for (int i = 0; i < U; ++i) {
         const int slot = org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i;
         token[i] = real_token(org.box, slot < org.box.n ? slot : org.box.n > 0 ? org.box.n - 1 : 0);
-        in[i] = Chunks<IN32>{};
+        in[i].w = 0;
         if (slot < org.box.n) in[i] = load_row<IN32>(x0 + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r, u);
     }
     // the group's entries: its planes' and rows' are runs of the table, its columns' each a run and as many (1, 0) as there are pairs left
@@ -344,38 +359,43 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 }
 
 // ---- the gradient -------------------------------------------------------------------------------
-// A workgroup takes 32 tokens at a time of HC heads (of one head, always the same, if they have weights of their own), reads the rows of all
-// of them at once and their cosines and sines once, and keeps its lanes' share of dweight in registers; the workgroups' sums are
-// added up by a second kernel, in a fixed order.
-template <bool F32, bool HALVES, int HC>
+// A workgroup takes 32 tokens of HC heads at a time, requests the rows of all of them at once and reads their cosines and sines once.  Its
+// lanes' share of dweight stays in registers, that of each head (OWN: the workgroup's heads are then always the same) or one
+// for all; the workgroups' sums are added up by a second kernel, in a fixed order.  (Requesting the next rows before these are worked
+// on takes all registers and gains nothing: 720p 455 us, 450 without.)
+template <bool F32, bool HALVES, int HC, bool OWN, bool PAST>
 __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, Rows dx, Turning k, float* __restrict__ partial,
                                                               int tokens, int heads, int batches, int workgroups) {
-    __shared__ float red[4][128];
+    constexpr int SUMS = OWN ? HC : 1;
+    __shared__ float red[4][SUMS][128];
     const int u = threadIdx.x & 7, row = threadIdx.x >> 3, parts = (int)((tokens + 31u) >> 5);
     const int group = blockIdx.x / workgroups, first = blockIdx.x - group * workgroups;
-    const int own_head = k.weight_head ? group : -1, per = own_head >= 0 ? 1 : (heads + HC - 1) / HC;
+    const int per = OWN ? 1 : (heads + HC - 1) / HC;
     const long long items = (long long)batches * parts * per;               // (batch, token part, heads)
-    Pairs dw;
+    Pairs dw[SUMS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw.a[i] = dw.b[i] = 0.0f;
+    for (int j = 0; j < SUMS; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j].a[i] = dw[j].b[i] = 0.0f;
     for (long long item = first; item < items; item += workgroups) {
         const long long bp = item / per;
-        const int h0 = own_head >= 0 ? own_head : (int)(item - bp * per) * HC, b = (int)(bp / parts);
-        const int n = (int)(bp - (long long)b * parts) * 32 + row, last = own_head >= 0 ? h0 + 1 : heads;
+        const int h0 = (OWN ? group : (int)(item - bp * per)) * HC, b = (int)(bp / parts), n = (int)(bp - (long long)b * parts) * 32 + row;
         if (n >= tokens) continue;
         Chunks<F32> cx[HC], cy[HC];
 #pragma unroll
         for (int i = 0; i < HC; ++i)
-            if (h0 + i < last) {
+            if (h0 + i < heads) {
                 cx[i] = load_row<F32>(x.at(b, h0 + i, n), u);
                 cy[i] = load_row<F32>(dy.at(b, h0 + i, n), u);
             }
         const Turn turn = load_turn<F32, HALVES>(k, b, n, u);
-        const Pairs w = load_weight<F32, HALVES>(k, h0, u);                       // of all of them, or of the one
+        Pairs w = load_weight<F32, HALVES>(k, h0, u);
 #pragma unroll
         for (int i = 0; i < HC; ++i) {
-            if (h0 + i >= last) break;
+            if (h0 + i >= heads) break;
+            if (OWN && i > 0) w = load_weight<F32, HALVES>(k, h0 + i, u);
             const Pairs xv = unpack<F32, HALVES>(cx[i]), g0 = unpack<F32, HALVES>(cy[i]);
+            Pairs& sum = dw[OWN ? i : 0];
             const float r = inverse_rms(k, xv);
             Pairs g;
             float dot = 0.0f;
@@ -383,8 +403,8 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             for (int m = 0; m < 8; ++m) {
                 const float ga = __builtin_fmaf(g0.a[m], turn.c[m], g0.b[m] * turn.s[m]);
                 const float gb = __builtin_fmaf(g0.b[m], turn.c[m], -(g0.a[m] * turn.s[m]));
-                dw.a[m] = __builtin_fmaf(ga, xv.a[m] * r, dw.a[m]);
-                dw.b[m] = __builtin_fmaf(gb, xv.b[m] * r, dw.b[m]);
+                sum.a[m] = __builtin_fmaf(ga, xv.a[m] * r, sum.a[m]);
+                sum.b[m] = __builtin_fmaf(gb, xv.b[m] * r, sum.b[m]);
                 g.a[m] = ga * w.a[m];
                 g.b[m] = gb * w.b[m];
                 dot = __builtin_fmaf(g.a[m], xv.a[m], __builtin_fmaf(g.b[m], xv.b[m], dot));
@@ -396,26 +416,32 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
                 d.a[m] = r * __builtin_fmaf(-xv.a[m], back, g.a[m]);
                 d.b[m] = r * __builtin_fmaf(-xv.b[m], back, g.b[m]);
             }
-            store_row<F32, F32, HALVES>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
+            store_row<F32, F32, HALVES, PAST>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
         }
     }
     if (!partial) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int j = 0; j < SUMS; ++j) {
 #pragma unroll
-        for (int off = 8; off < 64; off <<= 1) {
-            dw.a[i] += __shfl_xor(dw.a[i], off);
-            dw.b[i] += __shfl_xor(dw.b[i], off);
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int off = 8; off < 64; off <<= 1) {
+                dw[j].a[i] += __shfl_xor(dw[j].a[i], off);
+                dw[j].b[i] += __shfl_xor(dw[j].b[i], off);
+            }
+        if ((threadIdx.x & 63) < 8) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) red[threadIdx.x >> 6][j][channel_of<F32>(u, i)] = slot_of<HALVES>(dw[j], i);
         }
-    if ((threadIdx.x & 63) < 8) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) red[threadIdx.x >> 6][channel_of<F32>(u, i)] = slot_of<HALVES>(dw, i);
     }
     __syncthreads();
-    if (threadIdx.x < 128) {
-        const int c = threadIdx.x;
-        partial[(long long)blockIdx.x * 128 + c] = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
-    }
+    if (threadIdx.x < 128)
+#pragma unroll
+        for (int j = 0; j < SUMS; ++j) {                     // of a head its workgroups' sums follow each other
+            const int c = threadIdx.x, head = group * HC + j;
+            if (OWN && head >= heads) break;
+            partial[((long long)(OWN ? head : 0) * workgroups + first) * 128 + c] = (red[0][j][c] + red[1][j][c]) + (red[2][j][c] + red[3][j][c]);
+        }
 }
 // Eight channels a workgroup, 32 slices of the n partial sums
 __global__ __launch_bounds__(256) void sum_partials_kernel(const float* __restrict__ partial, float* __restrict__ out, int n) {
@@ -528,9 +554,15 @@ static Turning turning_of(const Geom& g, const fps_norm* norm, const fps_rotatio
     k.rc_row = reciprocal(g.W);
     return k;
 }
+// Input and output together beyond the Infinity Cache's 256 MB: the output does not push out what is there.  720p 303 -> 291 us, its gradient
+// 462 -> 450; of 480p, which the cache holds for what reads it next, 43.6 -> 39.4.
+static bool beyond_caches(const fps_view& x, const fps_view& y) {
+    const long long n = (long long)x.B * x.heads * x.rows * kHeadDim;
+    return n * ((x.dt == FPS_OUT_F32 ? 4 : 2) + (y.dt == FPS_OUT_F32 ? 4 : 2)) > (256LL << 20);
+}
 static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_PAIRS_HALVES; }
 
-constexpr int kHeads = 8, kBwdHeads = 4;                    // of a workgroup
+constexpr int kHeads = 8, kBwdHeads = 4, kBwdWorkgroups = 1024, kOwnHeads = 1, kOwnWorkgroups = 4096;
 
 // f(bool constants...) for run-time truth values
 template <typename F> static void with(bool a, F&& f) { if (a) f(std::true_type{}); else f(std::false_type{}); }
@@ -544,10 +576,15 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     const int parts = few ? x.heads : (x.heads + kHeads - 1) / kHeads;
     const long long grid = blocks * x.B * parts;
     if (grid > 0x7FFFFFFF) { set_error("more rows than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
-    with(x.dt == FPS_OUT_F32, [&](auto in32) { with(y.dt == FPS_OUT_F32, [&](auto out32) { with(halves(rot), [&](auto hv) { with(few, [&](auto one) {
-        constexpr int HC = decltype(one)::value ? 1 : kHeads;
-        norm_rotate_kernel<decltype(in32)::value, decltype(out32)::value, decltype(hv)::value, HC>
-            <<<(int)grid, 256, 0, st>>>(rows_of(x), rows_of(y), k, tokens, x.heads, parts);
+    const bool past = beyond_caches(x, y);
+    with(x.dt == FPS_OUT_F32, [&](auto in32) { with(y.dt == FPS_OUT_F32, [&](auto out32) { with(halves(rot), [&](auto hv) { with(past, [&](auto pa) {
+        auto launch = [&](auto hc) {
+            constexpr int HC = decltype(hc)::value;
+            norm_rotate_kernel<decltype(in32)::value, decltype(out32)::value, decltype(hv)::value, HC, HC != 1 && decltype(pa)::value>
+                <<<(int)grid, 256, 0, st>>>(rows_of(x), rows_of(y), k, tokens, x.heads, parts);
+        };
+        if (few) launch(Count<1>{});
+        else     launch(Count<kHeads>{});
     }); }); }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate launch");
@@ -590,11 +627,11 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");
 }
 
-// Workgroups of the gradient for each head, or for all where they share a weight
+// Workgroups of the gradient for each group of heads that have weights of their own, or for all where they share one
 static int bwd_workgroups(const Geom& g, int heads, bool per_head) {
-    const int batches = g.BH / heads;
-    const long long parts = ((long long)g.T * g.H * g.W + 31) / 32, items = parts * batches * (per_head ? 1 : (heads + kBwdHeads - 1) / kBwdHeads);
-    const long long most = per_head ? (1024 + heads - 1) / heads : 1024;
+    const long long parts = ((long long)g.T * g.H * g.W + 31) / 32 * (g.BH / heads);
+    const int at_once = per_head ? kOwnHeads : kBwdHeads, groups = (heads + at_once - 1) / at_once;
+    const long long items = per_head ? parts : parts * groups, most = per_head ? (kOwnWorkgroups + groups - 1) / groups : kBwdWorkgroups;
     return (int)(items < most ? items : most);
 }
 size_t norm_rotate_bwd_bytes(const Geom& g, int heads, bool per_head) {
@@ -604,13 +641,13 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
                            const fps_view& dx, float* dweight, float* partial, hipStream_t st) {
     const Turning k = turning_of(g, norm, rot);
     const bool per_head = norm && norm->per_head && norm->weight;
-    const int n = bwd_workgroups(g, x.heads, per_head), sums = per_head ? x.heads : 1;
+    const int n = bwd_workgroups(g, x.heads, per_head), grid = n * (per_head ? (x.heads + kOwnHeads - 1) / kOwnHeads : 1);
     if (!dweight) partial = nullptr;
-    with(x.dt == FPS_OUT_F32, [&](auto f32) { with(halves(rot), [&](auto hv) { with(per_head, [&](auto one) {
-        norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value, decltype(one)::value ? 1 : kBwdHeads>
-            <<<n * sums, 256, 0, st>>>(rows_of(x), rows_of(dy), rows_of(dx), k, partial, x.rows, x.heads, x.B, n);
-    }); }); });
-    if (dweight) sum_partials_kernel<<<16 * sums, 256, 0, st>>>(partial, dweight, n);
+    with(x.dt == FPS_OUT_F32, [&](auto f32) { with(halves(rot), [&](auto hv) { with(per_head, [&](auto own) { with(beyond_caches(x, dx), [&](auto pa) {
+        norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value, decltype(own)::value ? kOwnHeads : kBwdHeads, decltype(own)::value, decltype(pa)::value>
+            <<<grid, 256, 0, st>>>(rows_of(x), rows_of(dy), rows_of(dx), k, partial, x.rows, x.heads, x.B, n);
+    }); }); }); });
+    if (dweight) sum_partials_kernel<<<16 * (per_head ? x.heads : 1), 256, 0, st>>>(partial, dweight, n);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_bwd launch");
 }
