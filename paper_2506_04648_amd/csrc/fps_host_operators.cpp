@@ -264,8 +264,7 @@ int fps_mx4_linear(const fps_view* x, const void* w, const float* bias, const fp
         set_error("workspace of %zu bytes, %zu needed", workspace_bytes, mx4_bytes(M, K));
         return FPS_ERR_WORKSPACE;
     }
-    FPS_TRY(launch_mx4_quantize(*x, workspace, (hipStream_t)stream));
-    return launch_mx4_matmul((int)K, workspace, w, bias, *y, (hipStream_t)stream);
+    return launch_mx4_linear(*x, w, bias, *y, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

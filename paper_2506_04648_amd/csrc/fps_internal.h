@@ -204,6 +204,7 @@ int launch_dequantize(const Geom& g, const void* xq, const float* scales, int ro
 int launch_mx4_quantize(const fps_view& x, void* packed, hipStream_t st);
 int launch_mx4_dequantize(const void* packed, const fps_view& y, hipStream_t st);
 int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, const fps_view& y, hipStream_t st);
+int launch_mx4_linear(const fps_view& x, const void* w, const float* bias, const fps_view& y, void* workspace, hipStream_t st);
 
 int launch_copy(const void* in, void* out, long long bytes, hipStream_t st);
 int launch_mfma_rate(int workgroups, int iters, float* sink, hipStream_t st);

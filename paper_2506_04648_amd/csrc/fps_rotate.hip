@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 }
 
 // ---- into the packed operands -------------------------------------------------------------------
-// As quantize_tiles_kernel (and pack_bf16_kernel): a workgroup is one scale group of up to three blocks, held in
+// As quantize_tiles_kernel (and pack_bf16_kernel): a workgroup is one scale group of up to four blocks, held in
 // registers from the reading to the encoding; of larger groups a block, of which PASS 0 finds the maximum and PASS 1, which
 // reads x again, encodes.
 // A token's cosines and sines would be four times as many load instructions as its channels, and all the arithmetic is as long as the
@@ -609,6 +609,7 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
     else if (g.KBS == 2) whole(Count<2>{});
     else if (g.KBS == 3) whole(Count<3>{});
     else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
+        if (g.KBS == 4) return whole(Count<4>{});            // 512 tokens, 1024 threads: one pass instead of two and three launches less
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);

@@ -377,11 +377,16 @@ def attn_fwd(shape: Shape, window, prec, q, k, v, sq=None, sk=None, sv=None, vsc
 # ---- before and after the attention -------------------------------------------------------------
 def _here(*tensors):
     """Every tensor (None: left out) is on the current device, whose stream the call goes to."""
-    torch = _torch or _import_torch()
-    device = torch.cuda.current_device() if torch.cuda.is_available() else None
+    current = None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != device):
-            raise ValueError(f"a tensor on {t.device}, not on the current device (cuda:{device})")
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"a tensor on {t.device}, not on the current device")
+        if current is None:
+            current = (_torch or _import_torch()).cuda.current_device()
+        if t.get_device() != current:
+            raise ValueError(f"a tensor on {t.device}, not on the current device (cuda:{current})")
 
 
 def _whole(t, dtype, numel, name):
