@@ -68,7 +68,7 @@ struct Matrix {
     }
 };
 
-// the product of matrices that fill the GPU with 256 x 256 tiles (fps_mx4_matmul.hip)
-int launch_mx4_large(const void* a, const void* b, int K, const float* bias, const fps_view& y, hipStream_t st);
+// the product in tiles of 256 x 256 or 128 x 128, operands copied ahead into LDS (fps_mx4_matmul.hip); K below 2^30
+int launch_mx4_tiles(int edge, const void* a, const void* b, int K, const float* bias, const fps_view& y, hipStream_t st);
 
 }  // namespace fps

@@ -149,19 +149,18 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Packed p, Matrix y,
 }
 
 // ---- products -----------------------------------------------------------------------------------
-// A wave takes 32 MT rows and 32 NT columns and reads the operands straight into the matrix instructions' registers, the next step's
-// before it multiplies this one's.  A workgroup is WM x WN of them side by side, which share operands in the L1, times KW that share the
-// steps of K and add up their sums in LDS.  The result's transpose is computed, so that a lane's four consecutive registers are
-// four columns of a row.
+// A workgroup of KW waves takes 32 MT rows and 32 NT columns; its waves share the steps of K, read the operands straight into the matrix
+// instructions' registers, the next step's before they multiply this one's, and add up their sums in LDS.  The result's transpose is
+// computed, so that a lane's four consecutive registers are four columns of a row.
 __device__ __forceinline__ v8i operand(const uint4& c) { return v8i{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}; }
 
-template <int MT, int NT, int WM, int WN, int KW, bool F32>
-__global__ __launch_bounds__(64 * WM * WN * KW) void mx4_matmul_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, int columns) {
+template <int MT, int NT, int KW, bool F32>
+__global__ __launch_bounds__(64 * KW) void mx4_matmul_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, int columns) {
     constexpr int PITCH = 36, T = KW < 4 ? 64 * KW : 256;    // floats: rows 16 bytes further along the banks; threads that add up
-    __shared__ __attribute__((aligned(16))) float red[WM * WN][KW][32][PITCH];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kw = wave % KW, mn = wave / KW;
-    const int mt0 = (blockIdx.x / columns * WM + mn / WN) * MT, nt0 = (blockIdx.x % columns * WN + mn % WN) * NT;
-    const int M = y.all_rows(), N = y.all_cols(), h = lane >> 5, tid = threadIdx.x - mn * 64 * KW, out_n = 4 * (tid & 7);
+    __shared__ __attribute__((aligned(16))) float red[KW][32][PITCH];
+    const int lane = threadIdx.x & 63, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int mt0 = blockIdx.x / columns * MT, nt0 = blockIdx.x % columns * NT;
+    const int M = y.all_rows(), N = y.all_cols(), h = lane >> 5, out_n = 4 * (threadIdx.x & 7);
     v16f acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -231,20 +230,20 @@ __global__ __launch_bounds__(64 * WM * WN * KW) void mx4_matmul_kernel(Packed a,
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            if (i + j > 0 && KW > 1) __syncthreads();        // a wave alone: its LDS instructions keep their order
+            if (i + j > 0) __syncthreads();
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4*>(&red[mn][kw][lane & 31][8 * q + 4 * h]) =
+                *reinterpret_cast<float4*>(&red[kw][lane & 31][8 * q + 4 * h]) =
                     make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-            if (KW > 1) __syncthreads();
+            __syncthreads();
 #pragma unroll
             for (int t0 = 0; t0 < 256; t0 += T) {
-                const int t = t0 + tid, m = t >> 3, row_at = (mt0 + i) * 32 + m, col = (nt0 + j) * 32 + out_n;
+                const int t = t0 + threadIdx.x, m = t >> 3, row_at = (mt0 + i) * 32 + m, col = (nt0 + j) * 32 + out_n;
                 if (t >= 256 || row_at >= M || col >= N) continue;
-                float4 s = *reinterpret_cast<const float4*>(&red[mn][0][m][out_n]);
+                float4 s = *reinterpret_cast<const float4*>(&red[0][m][out_n]);
 #pragma unroll
                 for (int k = 1; k < KW; ++k) {
-                    const float4 o = *reinterpret_cast<const float4*>(&red[mn][k][m][out_n]);
+                    const float4 o = *reinterpret_cast<const float4*>(&red[k][m][out_n]);
                     s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
                 }
                 const float v[4] = {s.x + add[j][0], s.y + add[j][1], s.z + add[j][2], s.w + add[j][3]};
@@ -271,7 +270,7 @@ __global__ __launch_bounds__(64 * WM * WN * KW) void mx4_matmul_kernel(Packed a,
 }
 
 // ---- launches -----------------------------------------------------------------------------------
-// Fewer than 1024 tiles' steps: a quarter of a step a wave, and four times as many waves.  851 x 1536 in bf16 7.2 -> 0 us.
+// Fewer than 1024 tiles' steps: a quarter of a step a wave, and four times as many waves.  851 x 1536 in bf16 7.2 -> 3.7 us.
 int launch_mx4_quantize(const fps_view& v, void* packed, hipStream_t st) {
     const Matrix x(v);
     const Packed p(packed, x.all_rows(), x.all_cols());
@@ -301,38 +300,39 @@ int launch_mx4_dequantize(const void* packed, const fps_view& v, hipStream_t st)
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_dequantize launch");
 }
 
-template <int MT, int NT, int WM, int WN, int KW>
+template <int MT, int NT, int KW>
 static int launch_direct(const Packed& a, const Packed& b, const float* bias, const fps_view& v, hipStream_t st) {
-    const int columns = (b.tiles + NT * WN - 1) / (NT * WN);
-    const long long grid = (long long)((a.tiles + MT * WM - 1) / (MT * WM)) * columns;
+    const int columns = (b.tiles + NT - 1) / NT;
+    const long long grid = (long long)((a.tiles + MT - 1) / MT) * columns;
     if (grid > 0x7FFFFFFF) { set_error("more tiles than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
-    constexpr int TH = 64 * WM * WN * KW;
-    if (v.dt == FPS_OUT_F32) mx4_matmul_kernel<MT, NT, WM, WN, KW, true><<<(int)grid, TH, 0, st>>>(a, b, bias, Matrix(v), columns);
-    else                     mx4_matmul_kernel<MT, NT, WM, WN, KW, false><<<(int)grid, TH, 0, st>>>(a, b, bias, Matrix(v), columns);
+    if (v.dt == FPS_OUT_F32) mx4_matmul_kernel<MT, NT, KW, true><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v), columns);
+    else                     mx4_matmul_kernel<MT, NT, KW, false><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v), columns);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");
 }
 
+// Which product.  us of the product alone, rows x K x columns:
+//   straight into registers (tiles of 32, K shared by 4 / 8 waves) against tiles of 128 by way of LDS, of which there are
+//     1 x 5120 x 30720     13.8 / 13.8    14.9   240       300 x 1536 x 4608     6.1 /  7.6     6.6   108
+//     128 x 5120 x 5120     7.4 /  7.8    11.5    40       64 x 5120 x 15360    12.2 / 13.4    12.8   120
+//     96 x 20480 x 5120    18.3 / 20.0    34.3    40       400 x 1536 x 4608     7.0 /  9.6     6.7   144
+//     256 x 5120 x 5120    10.9 / 11.6    12.1    80       33 x 5120 x 30720    25.5 / 25.1    15.4   240
+//     1 x 20480 x 5120     12.4 / 11.7     -              1024 x 5120 x 5120    35.7 / 38.1    20.8   320
+//   so those of 128 from 112 of them on, with more rows than 32; eight waves only for few tiles and a long K;
+//   tiles of 256, one a CU at a time, against tiles of 128, two a CU that take 1.7 of the time together (3.4 for 5 where there are many):
+//     2048 x 5120 x 5120    36.9   32.4                     32760 x 1536 x 1536  46.9   48.5
+//     4255 x 1536 x 4608    29.3   22.2                     8192 x 5120 x 5120    108    116
+//     8000 x 1536 x 1536    18.4   17.2                     75600 x 5120 x 5120   965   1088
+//   which the rounds of 256 tiles that the CUs make tell apart.
 int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, const fps_view& v, hipStream_t st) {
     const Packed pa(a, (long long)v.B * v.rows, K), pb(b, (long long)v.heads * v.cols, K);
-#ifdef FPS_MX4_VARIANT
-    switch (FPS_MX4_VARIANT) {
-        case 0: return launch_mx4_large(a, b, K, bias, v, st);
-        case 1: return launch_direct<2, 2, 2, 2, 1>(pa, pb, bias, v, st);
-        case 2: return launch_direct<2, 2, 1, 1, 4>(pa, pb, bias, v, st);
-        case 3: return launch_direct<2, 2, 2, 1, 2>(pa, pb, bias, v, st);
-        case 4: return launch_direct<1, 1, 1, 1, 8>(pa, pb, bias, v, st);
-        case 5: return launch_direct<1, 2, 1, 1, 8>(pa, pb, bias, v, st);
-        case 6: return launch_direct<1, 1, 1, 1, 4>(pa, pb, bias, v, st);
-        case 7: return launch_direct<2, 2, 1, 1, 8>(pa, pb, bias, v, st);
-        case 8: return launch_direct<1, 2, 1, 1, 4>(pa, pb, bias, v, st);
-        case 9: return launch_direct<2, 1, 1, 1, 8>(pa, pb, bias, v, st);
-        case 10: return launch_direct<2, 2, 2, 2, 2>(pa, pb, bias, v, st);
+    const long long in_256 = (pa.tiles + 7LL) / 8 * ((pb.tiles + 7LL) / 8), in_128 = (pa.tiles + 3LL) / 4 * ((pb.tiles + 3LL) / 4);
+    if (pa.tiles > 1 && in_128 >= 112 && pa.steps < (1 << 22)) {
+        const bool large = 34 * ((in_256 + 255) / 256) <= 10 * ((in_128 + 255) / 256) + 3;
+        return launch_mx4_tiles(large ? 256 : 128, a, b, K, bias, v, st);
     }
-#endif
-    if (pa.steps < (1 << 22) && (long long)((pa.tiles + 7) / 8) * ((pb.tiles + 7) / 8) >= 128) return launch_mx4_large(a, b, K, bias, v, st);
-    if (pa.tiles == 1) return launch_direct<1, 1, 1, 1, 8>(pa, pb, bias, v, st);
-    return launch_direct<2, 2, 1, 1, 4>(pa, pb, bias, v, st);
+    if (pa.steps >= 16 && (long long)pa.tiles * pb.tiles <= 256) return launch_direct<1, 1, 8>(pa, pb, bias, v, st);
+    return launch_direct<1, 1, 4>(pa, pb, bias, v, st);
 }
 
 int launch_mx4_linear(const fps_view& x, const void* w, const float* bias, const fps_view& v, void* workspace, hipStream_t st) {

@@ -13,12 +13,17 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kTileEdge = 256, kEdgeTiles = kTileEdge / kMxRows;
-constexpr int kHalf = kMxStepBytes / 2, kSlot = 2 * kEdgeTiles * kHalf, kSlots = 4;              // bytes; of 16 row tiles half a step
-constexpr int kScales = kSlots * kSlot, kScaleSlot = 2 * kEdgeTiles * kMxScaleBytes;               // behind them, two steps' scales
-constexpr int kPieces = kScales + 2 * kScaleSlot;
-constexpr int kBias = kTileEdge * 4;                                       // a tile's bias, for each wave
-constexpr int kPiecePitch = 64 * 2 + 16, kPiece = 32 * kPiecePitch;       // 32 rows of 64 columns in bf16, on their way out
+constexpr int kHalf = kMxStepBytes / 2, kSlots = 4;
+
+// A workgroup's tile is 64 W rows and columns, a wave's 32 W; its LDS, in bytes
+template <int W, bool F32>
+struct Tile {
+    static constexpr int EDGE = 64 * W, TILES = 2 * W;                        // of 32 rows, of each operand
+    static constexpr int SLOT = 2 * TILES * kHalf, SCALES = kSlots * SLOT, SCALE_SLOT = 2 * TILES * kMxScaleBytes;
+    static constexpr int PIECES = SCALES + 2 * SCALE_SLOT;                    // on the way out 32 rows of 128 bytes a wave, or of 64 so that
+    static constexpr int ROW = W == 4 || F32 ? 128 : 64, PITCH = ROW + 16, PIECE = 32 * PITCH;     // two workgroups have room on a CU
+    static constexpr int BIAS = PIECES + 4 * PIECE, BYTES = BIAS + (W == 4 && !F32 ? 4 * EDGE * 4 : 0);
+};
 
 struct TileMap { int tiles_m, tiles_n, total, workgroups; };
 
@@ -59,9 +64,12 @@ __device__ __forceinline__ Place place_of(const TileMap& t, int i) {
     return Place{8 * g + rem - col * down, col};
 }
 
-template <bool F32, bool HIDDEN>
-__global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, TileMap map) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kPieces + 4 * (kPiece + kBias)];
+template <int WT, bool F32, bool HIDDEN>
+__global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mx4_large_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, TileMap map) {
+    static_assert(!HIDDEN || (WT == 4 && !F32), "a result on its way among the next tile's multiplications is in bf16");
+    using L = Tile<WT, F32>;
+    constexpr int QUARTER = WT * WT, COPIES = 2 * WT;        // multiplications of 64 columns; copies of half a step, without scales
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[L::BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, h = lane >> 5;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -73,31 +81,31 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     int tile = xcd * per_xcd + (blockIdx.x >> 3);
     if (tile >= end) return;
 
-    // copying: where the step that is copied next lies; wave w copies operand w / 2's row tiles 4 (w % 2) ..
+    // copying: where the step that is copied next lies; wave w copies operand w / 2's row tiles WT (w % 2) .., and scales of four
     const Packed& mine = wave < 2 ? a : b;
     int copy_tile = tile, copy_step = 0;
-    const char* codes_at[4];                                 // of the four row tiles
+    const char* codes_at[WT];                                // of the row tiles
     const char* scales_at;                                   // of their scales,
     uint32_t scales_off;                                     // the lane's share of which is 16 bytes of tile lane / 16
     auto locate = [&]() __attribute__((always_inline)) {
         const Place p = place_of(map, copy_tile);
-        const int first = (wave < 2 ? p.m : p.n) * kEdgeTiles + 4 * (wave & 1);
+        const int all = (wave < 2 ? p.m : p.n) * L::TILES, first = all + WT * (wave & 1), four = WT == 4 ? first : all;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)                          // beyond the last row tile: the last one again
+        for (int i = 0; i < WT; ++i)                         // beyond the last row tile: the last one again
             codes_at[i] = (const char*)mine.codes + (long long)min_of(first + i, mine.tiles - 1) * steps * kMxStepBytes;
-        const int base = min_of(first, mine.tiles - 1);
+        const int base = min_of(four, mine.tiles - 1);
         scales_at = (const char*)mine.scales + (long long)base * steps * kMxScaleBytes;
-        scales_off = (uint32_t)(min_of(first + (lane >> 4), mine.tiles - 1) - base) * steps * kMxScaleBytes + 16 * (lane & 15);
+        scales_off = (uint32_t)(min_of(four + (lane >> 4), mine.tiles - 1) - base) * steps * kMxScaleBytes + 16 * (lane & 15);
     };
     locate();
     uint32_t lane_off = 16 * lane;
-    const uint32_t code_slots = lds0 + 4 * wave * kHalf, scale_slots = lds0 + kScales + 4 * wave * kMxScaleBytes;
-    // one of the eight copies of half a step: kilobyte n % 2 of row tile n / 2; par: parity of the step
+    const uint32_t code_slots = lds0 + WT * wave * kHalf, scale_slots = lds0 + L::SCALES + 4 * (WT == 4 ? wave : wave >> 1) * kMxScaleBytes;
+    // one of the copies of half a step: kilobyte n % 2 of row tile n / 2; par: parity of the step
     auto copy_codes = [&](int par, auto half_tag, auto n_tag) __attribute__((always_inline)) {
         constexpr int half = decltype(half_tag)::value, n = decltype(n_tag)::value, far = half * kHalf + (n & 1) * 1024;
-        copy_1k<far>(codes_at[n >> 1], lane_off, code_slots + par * (2 * kSlot), half * kSlot + (n >> 1) * kHalf + (n & 1) * 1024);
+        copy_1k<far>(codes_at[n >> 1], lane_off, code_slots + par * (2 * L::SLOT), half * L::SLOT + (n >> 1) * kHalf + (n & 1) * 1024);
     };
-    auto copy_scales = [&](int par) __attribute__((always_inline)) { copy_lanes(scales_at, scales_off, scale_slots + par * kScaleSlot); };
+    auto copy_scales = [&](int par) __attribute__((always_inline)) { copy_lanes(scales_at, scales_off, scale_slots + par * L::SCALE_SLOT); };
     // to the next step; behind the last tile of the result the last one's again, or what follows it, which nobody reads
     auto advance = [&]() __attribute__((always_inline)) {
         const bool more = ++copy_step < steps;
@@ -107,45 +115,48 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
             copy_tile += stride;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) codes_at[i] += (long long)by * kMxStepBytes;
+        for (int i = 0; i < WT; ++i) codes_at[i] += (long long)by * kMxStepBytes;
         scales_at += (long long)by * kMxScaleBytes;
         if (!more && copy_tile < end) locate();
     };
 
-    uint4 ca[2][4], cb[2][4];
-    uint32_t sa[4], sb[4], sa_next[4], sb_next[4];
+    uint4 ca[2][WT], cb[2][WT];
+    uint32_t sa[WT], sb[WT], sa_next[WT], sb_next[WT];
     const uint8_t *read_a, *read_b, *read_sa, *read_sb;
     auto read_by = [&](int l) __attribute__((always_inline)) {
-        read_a = lds + 4 * wm * kHalf + 16 * l;
-        read_b = lds + (kEdgeTiles + 4 * wn) * kHalf + 16 * l;
-        read_sa = lds + kScales + 4 * wm * kMxScaleBytes + 4 * l;
-        read_sb = lds + kScales + (kEdgeTiles + 4 * wn) * kMxScaleBytes + 4 * l;
+        read_a = lds + WT * wm * kHalf + 16 * l;
+        read_b = lds + (L::TILES + WT * wn) * kHalf + 16 * l;
+        read_sa = lds + L::SCALES + WT * wm * kMxScaleBytes + 4 * l;
+        read_sb = lds + L::SCALES + (L::TILES + WT * wn) * kMxScaleBytes + 4 * l;
     };
     read_by(lane);
-    // one of the eight operands of quarter q (0 or 1) of a slot, in the order of their use
+    // one of the operands of quarter q (0 or 1) of a slot, in the order of their use
     auto read = [&](int set, int slot, int q, int n) __attribute__((always_inline)) {
-        const int at_slot = slot * kSlot + q * 1024;
-        if (n == 1 || n > 4) ca[set][n > 4 ? n - 4 : 0] = *reinterpret_cast<const uint4*>(read_a + at_slot + (n > 4 ? n - 4 : 0) * kHalf);
-        else                 cb[set][n ? n - 1 : 0] = *reinterpret_cast<const uint4*>(read_b + at_slot + (n ? n - 1 : 0) * kHalf);
+        const int at_slot = slot * L::SLOT + q * 1024, i = n > WT ? n - WT : 0, j = n > 0 && n <= WT ? n - 1 : 0;
+        if (n == 1 || n > WT) ca[set][i] = *reinterpret_cast<const uint4*>(read_a + at_slot + i * kHalf);
+        else                  cb[set][j] = *reinterpret_cast<const uint4*>(read_b + at_slot + j * kHalf);
     };
     auto read_scales = [&](int slot, int i) __attribute__((always_inline)) {
-        sa_next[i] = *reinterpret_cast<const uint32_t*>(read_sa + slot * kScaleSlot + i * kMxScaleBytes);
-        sb_next[i] = *reinterpret_cast<const uint32_t*>(read_sb + slot * kScaleSlot + i * kMxScaleBytes);
+        sa_next[i] = *reinterpret_cast<const uint32_t*>(read_sa + slot * L::SCALE_SLOT + i * kMxScaleBytes);
+        sb_next[i] = *reinterpret_cast<const uint32_t*>(read_sb + slot * L::SCALE_SLOT + i * kMxScaleBytes);
     };
-    v16f acc[4][4];
-    auto multiply = [&](auto q_tag, int n, bool first) __attribute__((always_inline)) {     // rows 32 (n / 4) .., columns 32 (n % 4) ..
+    v16f acc[WT][WT];
+    auto multiply = [&](auto q_tag, int n, bool first) __attribute__((always_inline)) {     // rows 32 (n / WT) .., columns 32 (n % WT) ..
         constexpr int q = decltype(q_tag)::value, set = q & 1;
         const v16f zero = {};
-        const int i = n >> 2, j = n & 3;
+        const int i = n / WT, j = n % WT;
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(cb[set][j]), operand(ca[set][i]), first ? zero : acc[i][j], 4, 4, q,
                                                                     (int)sb[j], q, (int)sa[i]);
     };
 
-    // steps 0 and 1 of the sequence: nine copies a wave for the first half of a step, eight for the second
+    // steps 0 and 1 of the sequence: COPIES + 1 copies a wave for the first half of a step, COPIES for the second
     auto copy_half = [&](int par, auto half_tag) __attribute__((always_inline)) {
         copy_codes(par, half_tag, Count<0>{}); copy_codes(par, half_tag, Count<1>{}); copy_codes(par, half_tag, Count<2>{});
-        copy_codes(par, half_tag, Count<3>{}); copy_codes(par, half_tag, Count<4>{}); copy_codes(par, half_tag, Count<5>{});
-        copy_codes(par, half_tag, Count<6>{}); copy_codes(par, half_tag, Count<7>{});
+        copy_codes(par, half_tag, Count<3>{});
+        if constexpr (WT == 4) {
+            copy_codes(par, half_tag, Count<4>{}); copy_codes(par, half_tag, Count<5>{}); copy_codes(par, half_tag, Count<6>{});
+            copy_codes(par, half_tag, Count<7>{});
+        }
     };
     copy_scales(0);
     copy_half(0, Count<0>{});
@@ -154,20 +165,21 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     copy_scales(1);
     copy_half(1, Count<0>{});
     copy_half(1, Count<1>{});
-    meet<25>();
+    meet<3 * COPIES + 1>();
     int parity = 0;                                          // of the step: its slots are 2 parity and 2 parity + 1
 #pragma unroll
-    for (int n = 0; n < 8; ++n) read(0, 0, 0, n);
+    for (int n = 0; n < 2 * WT; ++n) read(0, 0, 0, n);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) read_scales(0, i);
+    for (int i = 0; i < WT; ++i) read_scales(0, i);
     const int M = y.all_rows(), N = y.all_cols();
-    // ---- a tile's way out: pieces of 32 rows and 64 (fp32: 32) columns by way of the wave's own part of the LDS, which gives rows of 128 bytes.
+    // ---- a tile's way out: pieces of 32 rows and 64 or 32 columns by way of the wave's own part of the LDS, which gives rows of 128 or 64 bytes.
     // A wave's LDS instructions are carried out in their order, so none of this waits for anything but what it reads.
-    constexpr int E = F32 ? 4 : 2, W = 16 / E, JJ = F32 ? 1 : 2;       // bytes an element, elements of a lane's chunk, j of a piece
+    constexpr int E = F32 ? 4 : 2, W = 16 / E, JJ = L::ROW / (32 * E), LANES = L::ROW / 16;    // bytes an element, elements of a lane's chunk,
+                                                                                             // blocks and chunks of a piece's row
     struct Piece { uint8_t* in; const uint8_t* out; int row; };
     auto piece_of = [&](int l) __attribute__((always_inline)) {
-        uint8_t* const piece = lds + kPieces + wave * kPiece;
-        return Piece{piece + (l & 31) * kPiecePitch + 4 * (l >> 5) * E, piece + (l >> 3) * kPiecePitch + 16 * (l & 7), l >> 3};
+        uint8_t* const piece = lds + L::PIECES + wave * L::PIECE;
+        return Piece{piece + (l & 31) * L::PITCH + 4 * (l >> 5) * E, piece + l / LANES * L::PITCH + 16 * (l % LANES), l / LANES};
     };
 
     // HIDDEN: the sums of the tile before, in bf16: registers 8 (4 i + j) + 2 q, + 1 are columns 8 q + 4 h .. of block (i, j)
@@ -185,7 +197,7 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
         const int i = k >> 1, j = 2 * (k & 1) + (n >> 2), q = n & 3, r = 8 * (4 * i + j) + 2 * q;
         *reinterpret_cast<uint2*>(at.in + ((n >> 2) * 32 + 8 * q) * 2) = make_uint2(sums[r], sums[r + 1]);
     };
-    auto from_piece = [&](const Piece& at, int t) __attribute__((always_inline)) { chunk[t & 1] = *reinterpret_cast<const uint4*>(at.out + 8 * t * kPiecePitch); };
+    auto from_piece = [&](const Piece& at, int t) __attribute__((always_inline)) { chunk[t & 1] = *reinterpret_cast<const uint4*>(at.out + 64 / LANES * t * L::PITCH); };
     auto store_chunk = [&](const Piece& at, int k, int t) __attribute__((always_inline)) {        // no branch, which would part the multiplications
         const int down = 32 * (k >> 1) + 8 * t;
         const uint32_t outside = (uint32_t)((done_rows - 1 - down - at.row) >> 31);
@@ -201,8 +213,8 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
         if (m < 4) { to_piece(at, k, 2 * m); to_piece(at, k, 2 * m + 1); }
         else from_piece(at, m - 4);
     };
-    uint8_t* const bias_out = lds + kPieces + 4 * kPiece + wave * kBias;
-    const uint32_t bias_slot = lds0 + kPieces + 4 * kPiece + wave * kBias;
+    uint8_t* const bias_out = lds + L::BIAS + wave * L::EDGE * 4;
+    const uint32_t bias_slot = lds0 + L::BIAS + wave * L::EDGE * 4;
 
     for (; tile < end; tile += stride) {
         const int l0 = lane_anew();
@@ -216,40 +228,42 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
             Piece at_piece;
             if (out) at_piece = piece_of(lane_anew());
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { sa[i] = sa_next[i]; sb[i] = sb_next[i]; }
+            for (int i = 0; i < WT; ++i) { sa[i] = sa_next[i]; sb[i] = sb_next[i]; }
             advance();                                       // before all else: behind a branch the multiplications would wait for it
             __builtin_amdgcn_sched_barrier(0);
             auto half = [&](auto h_tag) __attribute__((always_inline)) {
                 constexpr int hf = decltype(h_tag)::value;
                 const int slot = 2 * parity + hf, next = hf ? 2 * (parity ^ 1) : slot + 1;
 #pragma unroll
-                for (int n = 0; n < 16; ++n) {
+                for (int n = 0; n < QUARTER; ++n) {
                     multiply(Count<2 * hf>{}, n, first && hf == 0);
-                    if (n < 8) read(1, slot, 1, n);
+                    if (n < 2 * WT) read(1, slot, 1, n);
                     if (out) way_out(at_piece, 32 * hf + n);
                     if (out && hf == 0 && n == 0) {
-                        const int c = min_of(p.n * kTileEdge + 4 * lane_anew(), N - 4);
+                        const int c = min_of(p.n * L::EDGE + 4 * lane_anew(), N - 4);
                         copy_lanes((const char*)(bias ? bias : (const float*)b.scales) + (bias ? 4LL * c : 0), bias_slot);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 // The next slot has landed, of two more the copies go on; this one is read.  Behind the copies that are waited for there
                 // are the bias and the stores of a first step.
-                meet<17 + (out ? (hf ? 23 : 7) : 0)>();
+                meet<2 * COPIES + 1 + (out ? (hf ? 23 : 7) : 0)>();
                 auto copying = [&](auto n_tag) __attribute__((always_inline)) {
                     constexpr int n = decltype(n_tag)::value;
                     multiply(Count<2 * hf + 1>{}, n, false);
-                    if (n < 8) read(0, next, 0, n);
-                    else copy_codes(parity, h_tag, Count<(n & 7)>{});          // of the step after the next, into this slot
-                    if (n == 7 && !hf) copy_scales(parity);
-                    if (n >= 4 && n < 8 && hf) read_scales(parity ^ 1, n & 3);
+                    if (n < 2 * WT) read(0, next, 0, n);
+                    if constexpr (n >= QUARTER - COPIES) copy_codes(parity, h_tag, Count<n - QUARTER + COPIES>{});    // of the step after the next,
+                    if (n == QUARTER / 2 - 1 && !hf) copy_scales(parity);                                             // into this slot
+                    if (n >= WT && n < 2 * WT && hf) read_scales(parity ^ 1, n - WT);
                     if (out) way_out(at_piece, 32 * hf + 16 + n);
                     __builtin_amdgcn_sched_barrier(0);
                 };
                 copying(Count<0>{}); copying(Count<1>{}); copying(Count<2>{}); copying(Count<3>{});
-                copying(Count<4>{}); copying(Count<5>{}); copying(Count<6>{}); copying(Count<7>{});
-                copying(Count<8>{}); copying(Count<9>{}); copying(Count<10>{}); copying(Count<11>{});
-                copying(Count<12>{}); copying(Count<13>{}); copying(Count<14>{}); copying(Count<15>{});
+                if constexpr (WT == 4) {
+                    copying(Count<4>{}); copying(Count<5>{}); copying(Count<6>{}); copying(Count<7>{});
+                    copying(Count<8>{}); copying(Count<9>{}); copying(Count<10>{}); copying(Count<11>{});
+                    copying(Count<12>{}); copying(Count<13>{}); copying(Count<14>{}); copying(Count<15>{});
+                }
             };
             half(Count<0>{});
             half(Count<1>{});
@@ -262,7 +276,7 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
         step(std::true_type{});
         for (int s = 1; s < steps; ++s) step(std::false_type{});
 
-        const int row0 = p.m * kTileEdge + wm * 128, col0 = p.n * kTileEdge + wn * 128;
+        const int row0 = p.m * L::EDGE + wm * (L::EDGE / 2), col0 = p.n * L::EDGE + wn * (L::EDGE / 2);
         auto biased = [&](int i, int j, int q, float (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = acc[i][j][4 * q + k];
@@ -304,9 +318,9 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
         } else {
             const Piece at_piece = piece_of(lane);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < WT; ++i)
 #pragma unroll
-                for (int jj = 0; jj < 4; jj += JJ) {
+                for (int jj = 0; jj < WT; jj += JJ) {
 #pragma unroll
                     for (int j = jj; j < jj + JJ; ++j)
 #pragma unroll
@@ -320,9 +334,9 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
                                                 __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2)));
                         }
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
+                    for (int t = 0; t < LANES / 2; ++t) {
                         from_piece(at_piece, t);
-                        const int row = row0 + 32 * i + 8 * t + (lane >> 3), col = col0 + 32 * jj + W * (lane & 7);
+                        const int row = row0 + 32 * i + 64 / LANES * t + lane / LANES, col = col0 + 32 * jj + W * (lane % LANES);
                         if (row >= M || col >= N) continue;
                         char* dst = y.row(row) + y.column<E>(col);
                         if (col + W <= N) {
@@ -350,25 +364,35 @@ __global__ __launch_bounds__(256, 1) void mx4_large_kernel(Packed a, Packed b, c
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // no copy is on its way to LDS that is another workgroup's by then
 }
 
-int launch_mx4_large(const void* pa, const void* pb, int K, const float* bias, const fps_view& v, hipStream_t st) {
+template <int WT>
+static int launch_tiles(const void* pa, const void* pb, int K, const float* bias, const fps_view& v, hipStream_t st) {
     const Matrix y(v);
     const Packed a(pa, y.all_rows(), K), b(pb, y.all_cols(), K);
+    constexpr int EDGE = 64 * WT;
     TileMap map;
-    map.tiles_m = (y.all_rows() + kTileEdge - 1) / kTileEdge;
-    map.tiles_n = (y.all_cols() + kTileEdge - 1) / kTileEdge;
+    map.tiles_m = (y.all_rows() + EDGE - 1) / EDGE;
+    map.tiles_n = (y.all_cols() + EDGE - 1) / EDGE;
     const long long total = (long long)map.tiles_m * map.tiles_n;
     if (total > 0x0FFFFFFF) { set_error("more tiles than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
     map.total = (int)total;
-    map.workgroups = 256;
-    // The stores among the next tile's multiplications are of whole 16-byte chunks, at 32-bit offsets from a tile's first row; a
-    // batch whose elements do not follow each other is written between the tiles
-    const bool chunks = y.all_cols() % 8 == 0 && (y.stride_h | y.stride_r) % 16 == 0;
-    const bool near = y.stride_r < (1 << 22) && 128 * y.stride_r + (y.heads - 1) * y.stride_h + 2LL * y.cols < 0xFFFFFFF0LL;
-    if (v.dt == FPS_OUT_F32)                   mx4_large_kernel<true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-    else if (y.B == 1 && chunks && near)       mx4_large_kernel<false, true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-    else                                       mx4_large_kernel<false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    map.workgroups = WT == 4 ? 256 : 512;                    // one or two a CU, which stay
+    if constexpr (WT == 4) {
+        // The stores among the next tile's multiplications are of whole 16-byte chunks, at 32-bit offsets from a tile's first row; a
+        // batch whose elements do not follow each other is written between the tiles
+        const bool chunks = y.all_cols() % 8 == 0 && (y.stride_h | y.stride_r) % 16 == 0;
+        const bool near = y.stride_r < (1 << 22) && 128 * y.stride_r + (y.heads - 1) * y.stride_h + 2LL * y.cols < 0xFFFFFFF0LL;
+        if (v.dt == FPS_OUT_F32)             mx4_large_kernel<4, true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else if (y.B == 1 && chunks && near) mx4_large_kernel<4, false, true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else                                 mx4_large_kernel<4, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    } else {
+        if (v.dt == FPS_OUT_F32) mx4_large_kernel<2, true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else                     mx4_large_kernel<2, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+    }
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");
+}
+int launch_mx4_tiles(int edge, const void* a, const void* b, int K, const float* bias, const fps_view& y, hipStream_t st) {
+    return edge == 256 ? launch_tiles<4>(a, b, K, bias, y, st) : launch_tiles<2>(a, b, K, bias, y, st);
 }
 
 }  // namespace fps
