@@ -149,76 +149,43 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Packed p, Matrix y,
 }
 
 // ---- products -----------------------------------------------------------------------------------
-// A workgroup of KW waves takes 32 MT rows and 32 NT columns; its waves share the steps of K, read the operands straight into the matrix
+// A workgroup of KW waves takes 32 rows and 32 columns; its waves share the steps of K, read the operands straight into the matrix
 // instructions' registers, the next step's before they multiply this one's, and add up their sums in LDS.  The result's transpose is
 // computed, so that a lane's four consecutive registers are four columns of a row.
 __device__ __forceinline__ v8i operand(const uint4& c) { return v8i{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}; }
 
-template <int MT, int NT, int KW, bool F32>
-__global__ __launch_bounds__(64 * KW) void mx4_matmul_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, int columns) {
-    constexpr int PITCH = 36, T = KW < 4 ? 64 * KW : 256;    // floats: rows 16 bytes further along the banks; threads that add up
+template <int KW, bool F32>
+__global__ __launch_bounds__(64 * KW) void mx4_matmul_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y) {
+    constexpr int PITCH = 36;                                // floats: rows 16 bytes further along the banks
     __shared__ __attribute__((aligned(16))) float red[KW][32][PITCH];
-    const int lane = threadIdx.x & 63, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int mt0 = blockIdx.x / columns * MT, nt0 = blockIdx.x % columns * NT;
-    const int M = y.all_rows(), N = y.all_cols(), h = lane >> 5, out_n = 4 * (threadIdx.x & 7);
-    v16f acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    const uint4 *pa[MT], *pb[NT];
-    const uint32_t *ps[MT], *pt[NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {                           // tiles beyond the last: the last one again
-        const long long at = (long long)min_of(mt0 + i, a.tiles - 1) * a.steps;
-        pa[i] = a.codes + at * 256 + lane;
-        ps[i] = a.scales + at * 64 + lane;
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const long long at = (long long)min_of(nt0 + j, b.tiles - 1) * b.steps;
-        pb[j] = b.codes + at * 256 + lane;
-        pt[j] = b.scales + at * 64 + lane;
-    }
-    struct Operands { uint4 a[MT][4], b[NT][4]; uint32_t sa[MT], sb[NT]; };
+    const int lane = threadIdx.x & 63, kw = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int mt = blockIdx.x / b.tiles, nt = blockIdx.x - mt * b.tiles, m = threadIdx.x >> 3, col = nt * 32 + 4 * (threadIdx.x & 7);
+    const int M = y.all_rows(), N = y.all_cols();
+    const long long at_a = (long long)mt * a.steps, at_b = (long long)nt * b.steps;
+    const uint4 *pa = a.codes + at_a * 256 + lane, *pb = b.codes + at_b * 256 + lane;
+    const uint32_t *ps = a.scales + at_a * 64 + lane, *pt = b.scales + at_b * 64 + lane;
+    struct Operands { uint4 a[4], b[4]; uint32_t sa, sb; };
     auto fetch = [&](Operands& o, int s) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
+        for (int q = 0; q < 4; ++q) o.b[q] = pb[s * 256LL + q * 64];
+        o.sb = pt[s * 64LL];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o.b[j][q] = pb[j][s * 256 + q * 64];
-            o.sb[j] = pt[j][s * 64];
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) o.a[i][q] = pa[i][s * 256 + q * 64];
-            o.sa[i] = ps[i][s * 64];
-        }
+        for (int q = 0; q < 4; ++q) o.a[q] = pa[s * 256LL + q * 64];
+        o.sa = ps[s * 64LL];
     };
+    v16f acc = {};
     auto multiply = [&](const Operands& o) __attribute__((always_inline)) {
         auto quarter = [&](auto q_tag) __attribute__((always_inline)) {
             constexpr int q = decltype(q_tag)::value;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(o.b[j][q]), operand(o.a[i][q]), acc[i][j], 4, 4, q,
-                                                                                (int)o.sb[j], q, (int)o.sa[i]);
+            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(o.b[q]), operand(o.a[q]), acc, 4, 4, q, (int)o.sb, q, (int)o.sa);
         };
         quarter(Count<0>{}); quarter(Count<1>{}); quarter(Count<2>{}); quarter(Count<3>{});
     };
     Operands one, other;
     if (kw < a.steps) fetch(one, kw);
-    float add[NT][4];                                        // the bias of the thread's columns
+    float add[4];                                            // the bias of the thread's columns
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int col = (nt0 + j) * 32 + out_n + k;
-            add[j][k] = bias && col < N ? bias[col] : 0.0f;
-        }
+    for (int k = 0; k < 4; ++k) add[k] = bias && col + k < N ? bias[col + k] : 0.0f;
     for (int s = kw; s < a.steps; s += 2 * KW) {
         if (s + KW < a.steps) fetch(other, s + KW);
         multiply(one);
@@ -227,46 +194,35 @@ __global__ __launch_bounds__(64 * KW) void mx4_matmul_kernel(Packed a, Packed b,
         multiply(other);
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(&red[kw][lane & 31][8 * q + 4 * h]) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+    __syncthreads();
+    if (m >= 32 || mt * 32 + m >= M || col >= N) return;
+    float4 s = *reinterpret_cast<const float4*>(&red[0][m][4 * (threadIdx.x & 7)]);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            if (i + j > 0) __syncthreads();
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4*>(&red[kw][lane & 31][8 * q + 4 * h]) =
-                    make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-            __syncthreads();
-#pragma unroll
-            for (int t0 = 0; t0 < 256; t0 += T) {
-                const int t = t0 + threadIdx.x, m = t >> 3, row_at = (mt0 + i) * 32 + m, col = (nt0 + j) * 32 + out_n;
-                if (t >= 256 || row_at >= M || col >= N) continue;
-                float4 s = *reinterpret_cast<const float4*>(&red[0][m][out_n]);
-#pragma unroll
-                for (int k = 1; k < KW; ++k) {
-                    const float4 o = *reinterpret_cast<const float4*>(&red[k][m][out_n]);
-                    s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
-                }
-                const float v[4] = {s.x + add[j][0], s.y + add[j][1], s.z + add[j][2], s.w + add[j][3]};
-                char* dst = y.row(row_at) + y.column<F32 ? 4 : 2>(col);
-                const int left = N - col;
-                if (left >= 4) {
-                    if (F32) {
-                        __builtin_memcpy(dst, v, 16);
-                    } else {
-                        const uint2 o = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[0], v[1]}, bf16x2)),
-                                                   __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2)));
-                        __builtin_memcpy(dst, &o, 8);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (k < left) {
-                            if (F32) reinterpret_cast<float*>(dst)[k] = v[k];
-                            else     reinterpret_cast<__bf16*>(dst)[k] = (__bf16)v[k];
-                        }
-                }
-            }
+    for (int k = 1; k < KW; ++k) {
+        const float4 o = *reinterpret_cast<const float4*>(&red[k][m][4 * (threadIdx.x & 7)]);
+        s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+    }
+    const float v[4] = {s.x + add[0], s.y + add[1], s.z + add[2], s.w + add[3]};
+    char* dst = y.row(mt * 32 + m) + y.column<F32 ? 4 : 2>(col);
+    const int left = N - col;
+    if (left >= 4) {
+        if (F32) {
+            __builtin_memcpy(dst, v, 16);
+        } else {
+            const uint2 o = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[0], v[1]}, bf16x2)),
+                                       __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2], v[3]}, bf16x2)));
+            __builtin_memcpy(dst, &o, 8);
         }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < left) {
+                if (F32) reinterpret_cast<float*>(dst)[k] = v[k];
+                else     reinterpret_cast<__bf16*>(dst)[k] = (__bf16)v[k];
+            }
+    }
 }
 
 // ---- launches -----------------------------------------------------------------------------------
@@ -300,13 +256,12 @@ int launch_mx4_dequantize(const void* packed, const fps_view& v, hipStream_t st)
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_dequantize launch");
 }
 
-template <int MT, int NT, int KW>
+template <int KW>
 static int launch_direct(const Packed& a, const Packed& b, const float* bias, const fps_view& v, hipStream_t st) {
-    const int columns = (b.tiles + NT - 1) / NT;
-    const long long grid = (long long)((a.tiles + MT - 1) / MT) * columns;
+    const long long grid = (long long)a.tiles * b.tiles;
     if (grid > 0x7FFFFFFF) { set_error("more tiles than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
-    if (v.dt == FPS_OUT_F32) mx4_matmul_kernel<MT, NT, KW, true><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v), columns);
-    else                     mx4_matmul_kernel<MT, NT, KW, false><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v), columns);
+    if (v.dt == FPS_OUT_F32) mx4_matmul_kernel<KW, true><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v));
+    else                     mx4_matmul_kernel<KW, false><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v));
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");
 }
@@ -331,8 +286,8 @@ int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, co
         const bool large = 34 * ((in_256 + 255) / 256) <= 10 * ((in_128 + 255) / 256) + 3;
         return launch_mx4_tiles(large ? 256 : 128, a, b, K, bias, v, st);
     }
-    if (pa.steps >= 16 && (long long)pa.tiles * pb.tiles <= 256) return launch_direct<1, 1, 8>(pa, pb, bias, v, st);
-    return launch_direct<1, 1, 4>(pa, pb, bias, v, st);
+    if (pa.steps >= 16 && (long long)pa.tiles * pb.tiles <= 256) return launch_direct<8>(pa, pb, bias, v, st);
+    return launch_direct<4>(pa, pb, bias, v, st);
 }
 
 int launch_mx4_linear(const fps_view& x, const void* w, const float* bias, const fps_view& v, void* workspace, hipStream_t st) {

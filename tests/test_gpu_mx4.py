@@ -96,6 +96,10 @@ def test_every_quotient_near_a_tie_in_fp32():
 SIZES = [(1, 1, 1), (1, 64, 64), (1, 5120, 640), (2, 33, 100), (7, 160, 33), (32, 256, 256), (33, 300, 31), (40, 512, 512), (64, 1536, 96),
          (77, 100, 1000), (100, 2304, 372), (128, 128, 128), (255, 640, 257), (256, 256, 256), (300, 700, 520), (513, 1000, 384),
          (851, 1536, 640), (16, 9000, 64), (2000, 96, 2100), (1, 96, 5000), (1025, 2049, 1030)]
+# From 112 tiles of 128 x 128 on they are what is multiplied, one step of K or more, the last tile cut; tiles of 256 where they fill the CUs
+# better, up to several of them one after the other
+SIZES += [(33, 300, 15000), (1400, 1100, 1501), (1500, 64, 1496), (15000, 200, 1), (5000, 257, 4100)]
+SIZES += [(7000, 64, 2104), (7001, 300, 2103), (8200, 520, 4104), (6921, 1792, 2048), (12000, 256, 5128)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
@@ -118,7 +122,8 @@ def test_product(M, K, N):
         assert torch.equal(fps.mx4_linear(x.float(), b, N, bias=add, out_dtype=F32), y)
 
 
-@pytest.mark.parametrize("B,heads_in,heads_out,tokens", [(1, 2, 3, 45), (2, 4, 5, 31), (3, 1, 2, 200), (1, 5, 12, 700)])
+@pytest.mark.parametrize("B,heads_in,heads_out,tokens", [(1, 2, 3, 45), (2, 4, 5, 31), (3, 1, 2, 200), (1, 5, 12, 700), (2, 2, 12, 700), (1, 1, 17, 7000),
+                                                          (2, 3, 16, 3500)])
 def test_product_between_the_attentions_layouts(B, heads_in, heads_out, tokens):
     say("layouts", B, heads_in, heads_out, tokens)
     gen = torch.Generator(device=DEV).manual_seed(tokens)
@@ -136,7 +141,7 @@ def test_product_between_the_attentions_layouts(B, heads_in, heads_out, tokens):
     assert bool((three[:, :, 0] == 7).all()) and bool((three[:, :, 2] == 7).all())
 
 
-@pytest.mark.parametrize("M,K,N", [(1, 700, 96), (40, 700, 96), (600, 700, 520)])
+@pytest.mark.parametrize("M,K,N", [(1, 700, 96), (40, 700, 96), (600, 700, 520), (1400, 700, 1500), (7000, 300, 2104)])
 def test_not_finite_blocks_make_their_rows_and_columns_nan(M, K, N):
     gen = torch.Generator(device=DEV).manual_seed(3)
     x, w = rows_of(gen, M, K, BF16), rows_of(gen, N, K, BF16)
@@ -148,11 +153,11 @@ def test_not_finite_blocks_make_their_rows_and_columns_nan(M, K, N):
     assert bool(z[bad].isnan().all()) and torch.equal(z[~bad], y[~bad])
 
 
-@pytest.mark.parametrize("M", [1, 33, 300])
-def test_scales_of_very_different_size(M):
+@pytest.mark.parametrize("M,N", [(1, 96), (33, 96), (300, 96), (15000, 96), (7000, 2104)])
+def test_scales_of_very_different_size(M, N):
     """Blocks from 2^-100 to 2^60, products from 2^-127 to 2^120, in one row; the bound is on the magnitudes' sum."""
     gen = torch.Generator(device=DEV).manual_seed(4)
-    K, N = 640, 96
+    K = 640
     e = torch.linspace(-60, 55, K // 32, device=DEV).round()
     x = (rows_of(gen, M, K, F32) * torch.exp2(e).repeat_interleave(32)).to(BF16)
     w = (rows_of(gen, N, K, F32) * torch.exp2(e.flip(0) * 0.9).round(decimals=0).clamp_min(2.0 ** -60).repeat_interleave(32)).to(BF16)
@@ -161,10 +166,10 @@ def test_scales_of_very_different_size(M):
     assert op.within(y, want, bound, F32) <= 1
 
 
-def test_exact_sums():
+@pytest.mark.parametrize("M,K,N", [(513, 1792, 770), (1, 5120, 640), (1400, 1792, 1500), (7000, 1792, 2104)])
+def test_exact_sums(M, K, N):
     """Small whole numbers: every sum is exact, whatever its order."""
     gen = torch.Generator(device=DEV).manual_seed(5)
-    M, K, N = 513, 1792, 770
     pick = torch.tensor([0, 1, 2, 3, 4, 6], device=DEV)
     x = (pick[torch.randint(6, (M, K), generator=gen, device=DEV)] * (1 - 2 * torch.randint(2, (M, K), generator=gen, device=DEV))).to(BF16)
     w = (pick[torch.randint(6, (N, K), generator=gen, device=DEV)] * (1 - 2 * torch.randint(2, (N, K), generator=gen, device=DEV))).to(BF16)
@@ -187,15 +192,35 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(x.reshape(6, 640), y)
 
 
+def test_packed_matrix_and_rows_of_the_result_beyond_4_gib():
+    """600000 rows that repeat 96 of small whole numbers, whose sums are exact in any order; then a result with rows 2 MB apart."""
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    K, N, times = 16384, 256, 6250
+    m, w = (torch.randint(-2, 3, (n, K), generator=gen, device=DEV).to(BF16) for n in (96, N))
+    packed = fps.mx4_quantize(m.expand(times, 96, K))
+    assert packed.numel() > 1 << 32
+    want = (m.double() @ w.double().t()).to(BF16)
+    for n in (40, N):                                        # tiles of 128, tiles of 256
+        y = fps.mx4_matmul(packed, fps.mx4_quantize(w[:n].contiguous()), times * 96, n, K)
+        assert bool((y.view(times, 96, n) == want[:, :n]).all())
+    assert bool((fps.mx4_dequantize(packed, times * 96, K)[-96:] == m).all())
+    del packed
+    x, b = rows_of(gen, 7000, 64, BF16), fps.mx4_quantize(rows_of(gen, 2104, 64, BF16))
+    y = fps.mx4_linear(x, b, 2104)
+    far = torch.full((7000, 1 << 20), 7.0, dtype=BF16, device=DEV)
+    fps.mx4_linear(x, b, 2104, out=far[:, :2104])
+    assert torch.equal(far[:, :2104], y) and bool((far[:, 2104:2400] == 7).all())
+
+
 def test_another_stream_and_replayed_graphs_that_share_a_workspace():
     """Two graphs captured with one workspace, replayed one after the other on new inputs, against eager calls."""
     gen = torch.Generator(device=DEV).manual_seed(7)
     cases = []
     w = {}
-    for M, K, N in ((1, 512, 320), (300, 512, 640)):
+    for M, K, N in ((1, 512, 320), (300, 512, 640), (1400, 512, 1504), (7000, 512, 2104)):
         w[N] = fps.mx4_quantize(rows_of(gen, N, K, BF16))
         cases.append((rows_of(gen, M, K, BF16), N, torch.empty(M, N, dtype=BF16, device=DEV)))
-    workspace = torch.empty(fps.mx4_linear_bytes(300, 512), dtype=torch.uint8, device=DEV)
+    workspace = torch.empty(fps.mx4_linear_bytes(7000, 512), dtype=torch.uint8, device=DEV)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
