@@ -216,29 +216,34 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // kStaged (STAGED) they are brought into LDS first, for FP8 multiplied by the pair's weights: (x, y) -> (x A - y B, x C + y D).  (BF16
 // operands are, bit for bit, the packed bf16 tensor, and take the products in its order.)
 constexpr int kWhole = -1, kStaged = 1024;
-template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED>
+// Half of a wave's instructions find its tokens and stage the turns.  MANY: they are for kManyHeads heads, one after the other, of
+// which the next one's rows are on their way while one is worked on.
+constexpr int kManyHeads = 4;
+struct Units { int heads, parts, count; uint32_t rc; };      // heads of a workgroup, workgroups for all heads; groups (blocks) of a head
+template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED, bool MANY>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
                                                                            float* __restrict__ scales, int role, Geom g,
-                                                                           int heads) {
+                                                                           int heads, Units units) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
-    __shared__ uint32_t red[WAVES];
+        __shared__ uint32_t red[2][WAVES];
     __shared__ __attribute__((aligned(16))) float4 staged[STAGED ? kStaged : 1];
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     load_arguments<6>();
-    const int blk = blockIdx.x * NB + kb;
-    const BlockOrigin org = block_origin(g, blockIdx.x * NB);
-    const int bh = quotient((int)org.tile_lin, g.M, g.rc_m), b = bh / heads, head = bh - b * heads;
-    const int n0 = (int)(org.raster0 - (long long)bh * g.T * g.H * g.W);
-    const char* const x0 = x.at(b, head, n0);
+    const int bp = quotient(blockIdx.x, units.count, units.rc), b = bp / units.parts, head0 = (bp - b * units.parts) * units.heads;
+    const int group0 = (b * heads + head0) * units.count + (blockIdx.x - bp * units.count), last_head = MANY ? min_of(head0 + units.heads, heads) - 1 : head0;
+    const BlockOrigin org = block_origin(g, group0 * NB);
+    const int n0 = (int)(org.raster0 - (long long)(b * heads + head0) * g.T * g.H * g.W);
 
-    Chunks<IN32> in[U];
+    Chunks<IN32> ahead[U];                                   // the rows of the head to come
     Offset token[U];                                         // from the group's first; padding is zeros at the place of the last token
+    const char* from[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int slot = org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i;
         token[i] = real_token(org.box, slot < org.box.n ? slot : org.box.n > 0 ? org.box.n - 1 : 0);
-        in[i].w = 0;
-        if (slot < org.box.n) in[i] = load_row<IN32>(x0 + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r, u);
+        from[i] = x.at(b, head0, n0) + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r;
+        ahead[i].w = 0;
+        if (slot < org.box.n) ahead[i] = load_row<IN32>(from[i], u);
     }
     // the group's entries: its planes' and rows' are runs of the table, its columns' each a run and as many (1, 0) as there are pairs left
     const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         const int step = axis == 2 ? k.cw : c, to = axis == 0 ? 0 : axis == 1 ? of_t : of_t + of_h;
         const bool turns = org.box.n > 0 && (axis < 2 || q < k.cw);
         const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
-        const float* w = k.weight + head * k.weight_head + a;
+        const float* w = k.weight + head0 * k.weight_head + a;
         const float wa = k.weight ? w[0] : 1.0f, wb = k.weight ? w[HALVES ? 64 : 1] : 1.0f;
         constexpr int R = THREADS * NB / 64, L = 4;          // places at a time, loads at a time
         for (int first = threadIdx.x >> 6; first < places; first += L * R) {
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         }
     }
     if (STAGED) __syncthreads();
-    auto turned = [&](const Pairs& v, const Offset& d) __attribute__((always_inline)) {
+    auto turned = [&](const Pairs& v, const Offset& d, int head) __attribute__((always_inline)) {
         if (!STAGED) return weighted_turned(v, load_weight<IN32, HALVES>(k, head, u),
                                             load_turn<IN32, HALVES>(k, b, min_of(n0 + (d.t * g.H + d.h) * g.W + d.w, g.T * g.H * g.W - 1), u));
         Pairs y;
@@ -285,75 +290,87 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         }
         return y;
     };
-    Pairs y[U];                                              // without the norm's factor r of the row
-    float r[U];
-    uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
+    for (int head = head0; head <= last_head; ++head) {
+        const int group = group0 + (head - head0) * units.count, blk = group * NB + kb;
+        Chunks<IN32> now[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const Pairs v = unpack<IN32, HALVES>(in[i]);
-        y[i] = turned(v, token[i]);
-        r[i] = inverse_rms(k, v);
-        if (FP8 && PASS != 1) {
-            float m = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = max_magnitude(m, y[i].a[j], y[i].b[j]);
-            const uint32_t of_row = __float_as_uint(m * r[i]) & 0x7FFFFFFFu;                        // rounds like the largest product
-            top = top > of_row ? top : of_row;
+        for (int i = 0; i < U; ++i) {
+            now[i] = ahead[i];
+            if (MANY && head < last_head) {
+                from[i] += x.h;
+                if (org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i < org.box.n) ahead[i] = load_row<IN32>(from[i], u);
+            }
         }
-    }
-    char* const dst = (char*)xq + (long long)blk * (BS * 128 * (FP8 ? 1 : 2));
-    if constexpr (!FP8) {                                    // 8 channels are a chunk of 16 bytes
+        Pairs y[U];                                              // without the norm's factor r of the row
+        float r[U];
+        uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const Pairs v = unpack<IN32, HALVES>(now[i]);
+            y[i] = turned(v, token[i], head);
+            r[i] = inverse_rms(k, v);
+            if (FP8 && PASS != 1) {
+                float m = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max_magnitude(m, y[i].a[j], y[i].b[j]);
+                const uint32_t of_row = __float_as_uint(m * r[i]) & 0x7FFFFFFFu;                        // rounds like the largest product
+                top = top > of_row ? top : of_row;
+            }
+        }
+        char* const dst = (char*)xq + (long long)blk * (BS * 128 * (FP8 ? 1 : 2));
+        if constexpr (!FP8) {                                    // 8 channels are a chunk of 16 bytes
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int j = (tid >> 3) + THREADS / 8 * i;
+                const Pairs z = times(y[i], r[i]);
+                const bool real = org.slot0 + kb * BS + j < org.box.n;               // padding is 0, not -0
+                auto two = [&](int s) __attribute__((always_inline)) { return real ? pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)) : 0u; };
+                auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
+#pragma unroll
+                for (int m = 0; m < 16; m += IN32 ? 4 : 8) {
+                    const int c = channel_of<IN32>(u, m);
+                    char* at = dst + 16 * chunk(c >> 3) + 2 * (c & 7);
+                    if (IN32) *reinterpret_cast<uint2*>(at) = make_uint2(two(m), two(m + 2));
+                    else      *reinterpret_cast<uint4*>(at) = make_uint4(two(m), two(m + 2), two(m + 4), two(m + 6));
+                }
+            }
+            continue;
+        }
+        if (PASS == 1) {
+            top = __float_as_uint(scales[quotient(group, g.KBS, g.rc_kbs)]);
+        } else {
+            top = workgroup_max<WAVES>(top, red[(head - head0) & 1]);
+            if (PASS == 0) {
+                if (threadIdx.x == 0) atomicMax((uint32_t*)&scales[quotient(group, g.KBS, g.rc_kbs)], top);
+                continue;
+            }
+        }
+        const float amax = __uint_as_float(top), s = top == 0 ? 1.0f : amax / 448.0f;
+        if (PASS == kWhole && threadIdx.x == 0) scales[group] = s;
+        // a scale near the end of the range: its reciprocal would pass it
+        const float up = s < 0x1p-60f ? 0x1p64f : 1.0f, rs = 1.0f / (s * up);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int j = (tid >> 3) + THREADS / 8 * i;
-            const Pairs z = times(y[i], r[i]);
-            const bool real = org.slot0 + kb * BS + j < org.box.n;               // padding is 0, not -0
-            auto two = [&](int s) __attribute__((always_inline)) { return real ? pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)) : 0u; };
-            auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
+            const Pairs z = times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs);         // |x| <= amax: the product cannot reach the next code, 480
+            // the 16-byte chunk of channels 16 c16 ..
+            auto chunk = [&](int c16) {
+                return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
+            };
+            uint32_t o[4];
 #pragma unroll
-            for (int m = 0; m < 16; m += IN32 ? 4 : 8) {
-                const int c = channel_of<IN32>(u, m);
-                char* at = dst + 16 * chunk(c >> 3) + 2 * (c & 7);
-                if (IN32) *reinterpret_cast<uint2*>(at) = make_uint2(two(m), two(m + 2));
-                else      *reinterpret_cast<uint4*>(at) = make_uint4(two(m), two(m + 2), two(m + 4), two(m + 6));
+            for (int m = 0; m < 4; ++m) {
+                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
+                o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
+                o[m] = org.slot0 + kb * BS + j < org.box.n ? o[m] : 0u;              // padding is 0, not -0
             }
-        }
-        return;
-    }
-    if (PASS == 1) {
-        top = __float_as_uint(scales[quotient(blockIdx.x, g.KBS, g.rc_kbs)]);
-    } else {
-        top = workgroup_max<WAVES>(top, red);
-        if (PASS == 0) {
-            if (threadIdx.x == 0) atomicMax((uint32_t*)&scales[quotient(blockIdx.x, g.KBS, g.rc_kbs)], top);
-            return;
-        }
-    }
-    const float amax = __uint_as_float(top), s = top == 0 ? 1.0f : amax / 448.0f;
-    if (PASS == kWhole && threadIdx.x == 0) scales[blockIdx.x] = s;
-    // a scale near the end of the range: its reciprocal would pass it
-    const float up = s < 0x1p-60f ? 0x1p64f : 1.0f, rs = 1.0f / (s * up);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int j = (tid >> 3) + THREADS / 8 * i;
-        const Pairs z = times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs);         // |x| <= amax: the product cannot reach the next code, 480
-        // the 16-byte chunk of channels 16 c16 ..
-        auto chunk = [&](int c16) {
-            return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
-        };
-        uint32_t o[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
-            o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
-            o[m] = org.slot0 + kb * BS + j < org.box.n ? o[m] : 0u;              // padding is 0, not -0
-        }
-#pragma unroll
-        for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
-            const int c = channel_of<IN32>(u, 4 * m);
-            char* at = dst + 16 * chunk(c >> 4) + (c & 15);
-            if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
-            else      *reinterpret_cast<uint2*>(at) = make_uint2(o[m], o[(m + 1) & 3]);
+            for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
+                const int c = channel_of<IN32>(u, 4 * m);
+                char* at = dst + 16 * chunk(c >> 4) + (c & 15);
+                if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
+                else      *reinterpret_cast<uint2*>(at) = make_uint2(o[m], o[(m + 1) & 3]);
+            }
         }
     }
 }
@@ -590,20 +607,28 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate launch");
 }
 
-template <int BS, bool IN32, bool HALVES, bool STAGED>
+template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY>
 static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                            hipStream_t st) {
     // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
     // be more threads than a workgroup may have
     constexpr int TH = BS == 128 ? 512 : 128;
-    const int blocks = g.BH * g.M * g.KB, groups = g.BH * g.M * g.NS;
+    struct Launch { Units units; int grid; };
+    auto of_head = [&](int count, bool many) {
+        const int each = many ? kManyHeads : 1, parts = (heads + each - 1) / each;
+        return Launch{Units{each, parts, count, reciprocal(count)}, g.BH / heads * parts * count};
+    };
+    const Launch blocks = of_head(g.M * g.KB, MANY);
+    const int groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         return;
     }
     auto whole = [&](auto nb) {
         constexpr int NB = decltype(nb)::value, T = TH * NB > 1024 ? TH / 2 : TH;
-        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED><<<groups, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads);
+        constexpr bool many = MANY && T == TH;               // twice the rows a lane: no registers for the next head's
+        const Launch l = of_head(g.M * g.NS, many);
+        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
     };
     if (g.KBS == 1)      whole(Count<1>{});
     else if (g.KBS == 2) whole(Count<2>{});
@@ -611,8 +636,8 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
     else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
         if (g.KBS == 4) return whole(Count<4>{});            // 512 tokens, 1024 threads: one pass instead of two and three launches less
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED><<<blocks, TH, 0, st>>>(x, k, xq, scales, role, g, heads);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         amax_to_scale_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
 }
@@ -621,9 +646,19 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
                                int prec, void* xq, float* scales, hipStream_t st) {
     const Turning k = turning_of(g, norm, rot);
     const bool staged = (long long)g.Qt * k.ct + (long long)g.Qh * k.ch + (long long)g.Qw * (64 - k.ct - k.ch) <= kStaged;
-    with(g.BS == 128, [&](auto big) { with(x.dt == FPS_OUT_F32, [&](auto in32) { with(halves(rot), [&](auto hv) { with(staged, [&](auto sg) {
-        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value>(g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
-    }); }); }); });
+    // Several heads a workgroup where there are 1024 blocks of 128 slots or more (bf16, one weight for all: the staged turns hold
+    // it; fp32 rows leave no registers).  us with one head, with four: 480p of 12 heads 38.9, 32.7 (BF16 48.8, 43.8), 720p of 40 heads 247,
+    // 226 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12 heads, 540 blocks of 128, 9.6, 11.1
+    const bool many = staged && x.heads > 1 && !k.weight_head && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
+    auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn) {
+        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value>(
+            g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
+    };
+    with(g.BS == 128, [&](auto big) { with(halves(rot), [&](auto hv) {
+        if (x.dt == FPS_OUT_F32) with(staged, [&](auto sg) { launch(big, std::true_type{}, hv, sg, std::false_type{}); });
+        else if (many)           launch(big, std::false_type{}, hv, std::true_type{}, std::true_type{});
+        else                     with(staged, [&](auto sg) { launch(big, std::false_type{}, hv, sg, std::false_type{}); });
+    }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");
 }

@@ -156,6 +156,12 @@ OPERANDS = [
     dict(grid=(1, 2, 100), tile=(1, 2, 48), layout="fused", split=(2, 2, 60)),                 # turns that are not staged: one workgroup
     dict(grid=(2, 3, 150), tile=(1, 1, 128), weight="per_head", halves=True, split=(0, 0, 64)),   # of 128 and
     dict(grid=(1, 20, 130), tile=(1, 16, 64), heads=3, split=(0, 0, 40)),                      # in two passes
+    dict(grid=(9, 60, 70), tile=(1, 8, 16), heads=5, B=2, layout="fused"),                     # several heads a workgroup, the last of them
+    dict(grid=(9, 60, 70), tile=(2, 8, 16), heads=6, layout="gaps", B=2, tables=2, halves=True),    # fewer; two blocks,
+    dict(grid=(8, 60, 70), tile=(4, 16, 16), heads=7, layout="fused"),                         # two passes,
+    dict(grid=(9, 60, 70), tile=(3, 4, 4), heads=9, qtile=(1, 4, 4)),                          # blocks of 32
+    dict(grid=(9, 60, 70), tile=(8, 8, 8), heads=5, layout="fused"),                           # four blocks: one head
+    dict(grid=(9, 60, 70), tile=(1, 8, 16), heads=5, B=2, layout="fused", weight="per_head"),
 ]
 
 
