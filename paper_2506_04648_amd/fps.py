@@ -381,12 +381,11 @@ def _here(*tensors):
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
-            raise ValueError(f"a tensor on {t.device}, not on the current device")
-        if current is None:
+        device = t.get_device()                            # -1 on the host
+        if current is None and device >= 0:
             current = (_torch or _import_torch()).cuda.current_device()
-        if t.get_device() != current:
-            raise ValueError(f"a tensor on {t.device}, not on the current device (cuda:{current})")
+        if device < 0 or device != current:
+            raise ValueError(f"a tensor on {t.device}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
 
 
 def _whole(t, dtype, numel, name):
@@ -405,21 +404,23 @@ def _dtype_code(t):
 
 def _view(t, name) -> View:
     """[B, heads, tokens.., cols] of any strides; axes of tokens must follow each other in memory as in the shape."""
-    if t.dim() < 4:
-        raise ValueError(f"{name} must be [B, heads, tokens.., channels], not {tuple(t.shape)}")
     size, stride = t.shape, t.stride()
+    last = len(size) - 1
+    if last < 3:
+        raise ValueError(f"{name} must be [B, heads, tokens.., channels], not {tuple(size)}")
     rows, at = 1, 0
-    for n, s in zip(reversed(size[2:-1]), reversed(stride[2:-1])):
+    for i in range(last - 1, 1, -1):                       # two of these views are made a call: as little as it takes
+        n = size[i]
         if n == 1:
             continue
         if rows == 1:
-            at = s
-        elif s != at * rows:
+            at = stride[i]
+        elif stride[i] != at * rows:
             raise ValueError(f"{name}: the token axes of strides {stride[2:-1]} are not one axis")
         rows *= n
-    if stride[-1] != 1 and size[-1] > 1:
+    if stride[last] != 1 and size[last] > 1:
         raise ValueError(f"{name}: the channels must be contiguous")
-    return View(t.data_ptr(), _dtype_code(t), size[0], size[1], rows, size[-1], stride[0], stride[1], at)
+    return View(t.data_ptr(), _dtype_code(t), size[0], size[1], rows, size[last], stride[0], stride[1], at)
 
 
 def make_norm(weight=None, eps=1e-6) -> Norm:
