@@ -460,20 +460,22 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             partial[((long long)(OWN ? head : 0) * workgroups + first) * 128 + c] = (red[0][j][c] + red[1][j][c]) + (red[2][j][c] + red[3][j][c]);
         }
 }
-// Eight channels a workgroup, 32 slices of the n partial sums
-__global__ __launch_bounds__(256) void sum_partials_kernel(const float* __restrict__ partial, float* __restrict__ out, int n) {
-    __shared__ float red[32][9];
+// Eight channels a workgroup, 128 slices of the n partial sums: what bounds it is the loads that follow each other
+__global__ __launch_bounds__(1024) void sum_partials_kernel(const float* __restrict__ partial, float* __restrict__ out, int n) {
+    __shared__ float red[16][8];
     const int c = threadIdx.x & 7, slice = threadIdx.x >> 3, group = blockIdx.x >> 4, c0 = 8 * (blockIdx.x & 15);
     const float* p = partial + (long long)group * n * 128 + c0 + c;
     float s = 0.0f;
 #pragma unroll 8
-    for (int i = slice; i < n; i += 32) s += p[(long long)i * 128];
-    red[slice][c] = s;
+    for (int i = slice; i < n; i += 128) s += p[(long long)i * 128];
+#pragma unroll
+    for (int off = 8; off < 64; off <<= 1) s += __shfl_xor(s, off);
+    if ((threadIdx.x & 63) < 8) red[threadIdx.x >> 6][c] = s;
     __syncthreads();
     if (threadIdx.x < 8) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) t += red[i][threadIdx.x];
+        for (int i = 0; i < 16; ++i) t += red[i][threadIdx.x];
         out[group * 128 + c0 + threadIdx.x] = t;
     }
 }
@@ -683,7 +685,7 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
         norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value, decltype(own)::value ? kOwnHeads : kBwdHeads, decltype(own)::value, decltype(pa)::value>
             <<<grid, 256, 0, st>>>(rows_of(x), rows_of(dy), rows_of(dx), k, partial, x.rows, x.heads, x.B, n);
     }); }); }); });
-    if (dweight) sum_partials_kernel<<<16 * (per_head ? x.heads : 1), 256, 0, st>>>(partial, dweight, n);
+    if (dweight) sum_partials_kernel<<<16 * (per_head ? x.heads : 1), 1024, 0, st>>>(partial, dweight, n);
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_bwd launch");
 }
