@@ -287,9 +287,9 @@ typedef enum {
 
 /* Rotation by the token's place: pair p of token (t,h,w), (x,y) -> (x cos - y sin, x sin + y cos).  The first pairs_t pairs
  * turn with t, the next pairs_h with h, the next pairs_w with w; what is left of the 64 stays.  table: fp32 (device), (cos, sin)
- * of [T,pairs_t], then [H,pairs_h], then [W,pairs_w], not looked at if no pair turns; stride_b is the distance in floats between the tables of two batch
- * elements, even and not negative, 0 if they share one.  It is as long as the axes, not as the tokens: 20 KB at 720p, which stay in the caches
- * while the tokens pass. */
+ * of [T,pairs_t], then [H,pairs_h], then [W,pairs_w], not looked at if no pair turns; stride_b is the distance in floats between the
+ * tables of two batch elements, even and not negative, 0 if they share one.  It is as long as the axes, not as the tokens: 20 KB at
+ * 720p, which stay in the caches while the tokens pass. */
 typedef struct {
     const float* table;
     int64_t stride_b;
@@ -307,8 +307,8 @@ int fps_rotation_table_host(const fps_shape* shape, const fps_rotation* rot, con
 /* Norm, then rotation, in one pass.  x and y: [B,heads,T*H*W,128], tokens in raster order, bf16 or fp32 each; rows are 16-byte
  * aligned (strides are multiples of 8 elements in bf16, 4 in fp32).  norm or rot may be NULL: without that step.  Computed in
  * fp32 and rounded once, at the end.  y may be x itself (the same data, type and strides).  Of shape the grid, B and heads
- * count; its tile only has to be valid.  A row that holds an infinity or a NaN, or whose squares' sum passes fp32's
- * range, gives such values itself and leaves the other rows alone. */
+ * count; its tile only has to be valid.  A row that holds an infinity or a NaN gives such values itself and leaves the other rows
+ * alone; one whose squares' sum passes fp32's range (magnitudes about 2^64) counts as infinitely long and gives zeros. */
 int fps_norm_rotate(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
                     const fps_view* y, void* stream);
 

@@ -187,7 +187,7 @@ __device__ __forceinline__ Pairs times(const Pairs& y, float r) {
 }
 
 // ---- into the caller's layout -------------------------------------------------------------------
-// A wave takes eight tokens; each of its rows' cosines and sines are read once for HC heads.
+// A wave takes eight tokens, whose cosines and sines are read once for HC heads.
 template <bool IN32, bool OUT32, bool HALVES, int HC, bool PAST>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turning k, int tokens, int heads, int parts) {
     const int blocks = (int)((tokens + 31u) >> 5), bp = blockIdx.x / blocks;        // tokens fastest
@@ -581,7 +581,11 @@ static bool beyond_caches(const fps_view& x, const fps_view& y) {
 }
 static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_PAIRS_HALVES; }
 
-constexpr int kHeads = 8, kBwdHeads = 4, kBwdWorkgroups = 1024, kOwnHeads = 1, kOwnWorkgroups = 4096;
+// Heads a workgroup takes together.  us: forward, 720p of 40 heads, 480p of 12, 720p of 3: 2 292, 32.3, 20.3; 4 281, 31.4, 20.3; 8 286, 31.8,
+// 22.3; 16 294, 34.6, 24.7.  The gradient with one weight for all, with its second kernel: 2 519, 68, 40; 4 468, 58, 36; 8 476, 67, 36; with
+// weights of each head: 1 508, 70, 40; 2 469, 79, 51; 4 574, 119, 80.  Its workgroups, which stay: 512 468, 58.2, 36.7; 1024 468, 60.5, 35.4;
+// 2048 467, 65, 38; with weights of each head 2048 552, 72, 37; 4096 508, 70, 40; 8192 489, 74, 46.
+constexpr int kHeads = 4, kBwdHeads = 4, kBwdWorkgroups = 512, kOwnHeads = 1, kOwnWorkgroups = 4096;
 
 // f(bool constants...) for run-time truth values
 template <typename F> static void with(bool a, F&& f) { if (a) f(std::true_type{}); else f(std::false_type{}); }
@@ -591,7 +595,9 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     const Turning k = turning_of(g, norm, rot);
     const int tokens = x.rows;
     const long long blocks = (tokens + 31LL) / 32;
-    const bool few = blocks * x.B * x.heads < 4096;
+    // one head a workgroup, four: 128 tokens of 40 heads (160 parts of 32 rows) 3.2, 4.2 us; 1170 tokens of 40 heads (1480) 6.9, 6.5; 4255 of 12
+    // (1596) 7.6, 6.8; 7800 of 12 (2928) 11.4, 9.9
+    const bool few = blocks * x.B * x.heads < 1024;
     const int parts = few ? x.heads : (x.heads + kHeads - 1) / kHeads;
     const long long grid = blocks * x.B * parts;
     if (grid > 0x7FFFFFFF) { set_error("more rows than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }

@@ -106,6 +106,10 @@ def test_rows_with_infinities_and_nans_leave_the_others_alone():
     assert bool((z[rows].isnan() | z[rows].isinf()).any(-1).all())
     zero = fps.norm_rotate(c.shape, torch.zeros_like(c.x), c.norm, c.rotation)
     assert bool((zero == 0).all())
+    long = c.x.clone()
+    long[0, 1, 17] = long[0, 1, 17].sign() * 2.0 ** 65
+    z = fps.norm_rotate(c.shape, long, c.norm, c.rotation).reshape(c.x.shape)
+    assert bool((z[0, 1, 17] == 0).all()) and torch.equal(z[0, 2], y[0, 2]) and torch.equal(z[0, 1, :17], y[0, 1, :17])
 
 
 def test_offsets_beyond_32_bits():
