@@ -225,7 +225,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                                                                            float* __restrict__ scales, int role, Geom g,
                                                                            int heads, Units units) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
-        __shared__ uint32_t red[2][WAVES];
+    __shared__ uint32_t red[2][WAVES];                        // of one head and the next
     __shared__ __attribute__((aligned(16))) float4 staged[STAGED ? kStaged : 1];
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     load_arguments<6>();
@@ -306,6 +306,13 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
 #pragma unroll
         for (int i = 0; i < U; ++i) {
+            // a wave's rows of padding alone: tile (4,16,16), half of it outside the grid, 190 -> 172 us, BF16 of 480p 44.4 -> 41.3
+            if (org.slot0 + kb * BS + (__builtin_amdgcn_readfirstlane(tid >> 6) << 3) + THREADS / 8 * i >= org.box.n) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
+                r[i] = 1.0f;
+                continue;
+            }
             const Pairs v = unpack<IN32, HALVES>(now[i]);
             y[i] = turned(v, token[i], head);
             r[i] = inverse_rms(k, v);
