@@ -39,6 +39,13 @@ __device__ __forceinline__ Block<F32> load_block(const char* p, int n) {        
     return b;
 }
 
+// the scale of a block whose largest magnitude has the bits `top`
+struct BlockScale { uint32_t byte; float value; };
+__device__ __forceinline__ BlockScale block_scale(uint32_t top) {
+    const int e = (int)(top >> 23);
+    const uint32_t byte = e == 255 ? 255u : top == 0 ? 127u : e > 2 ? (uint32_t)(e - 2) : 0u;
+    return BlockScale{byte, __uint_as_float(e == 255 ? 0x3F800000u : byte == 0 ? 0x00400000u : byte << 23)};
+}
 // codes and scale byte of a block
 template <bool F32>
 __device__ __forceinline__ uint4 encode_block(const Block<F32>& b, uint32_t* byte) {
@@ -55,9 +62,9 @@ __device__ __forceinline__ uint4 encode_block(const Block<F32>& b, uint32_t* byt
             top = hi > top ? hi : top;
         }
     }
-    const int e = (int)(top >> 23);
-    *byte = e == 255 ? 255u : top == 0 ? 127u : e > 2 ? (uint32_t)(e - 2) : 0u;
-    const float scale = __uint_as_float(e == 255 ? 0x3F800000u : *byte == 0 ? 0x00400000u : *byte << 23);
+    const BlockScale s = block_scale(top);
+    const float scale = s.value;
+    *byte = s.byte;
     uint32_t o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -103,6 +110,96 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(Matrix x, uint4* __re
         if (QS == 1) reinterpret_cast<uint8_t*>(scales)[((long long)at * 64 + lane) * 4 + q] = (uint8_t)byte;
     }
     if (QS == 4) scales[(long long)at * 64 + lane] = word;
+}
+
+// The same for matrices beyond the caches, read past them, which then keep the codes for the product: four lanes hold a block, 16 of them the
+// 128 columns of a row, so that each load is whole lines (a lane's 64 bytes above are four loads of a line that has to stay); the codes
+// go by way of the wave's own part of the LDS, whose instructions are carried out in their order.
+template <bool F32>
+__global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(Matrix x, uint4* __restrict__ codes, uint32_t* __restrict__ scales, int steps,
+                                                                int waves) {
+    constexpr int E = F32 ? 4 : 2, WORDS = 2 * E, AT_ONCE = F32 ? 1 : 2, GROUP = 32 * 16 + 64, CODES = 8 * GROUP;     // 64 bytes: other banks
+    __shared__ __attribute__((aligned(16))) uint8_t stage[4][CODES + kMxScaleBytes];
+    const int wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (wave >= waves) return;
+    uint8_t* const mine = stage[threadIdx.x >> 6];
+    const int tile = wave / steps, step = wave - tile * steps, piece = lane & 3, blk = (lane >> 2) & 3, r4 = lane >> 4;
+    const int M = x.all_rows(), K = x.all_cols();
+    const char* row[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row[i] = x.row(min_of(tile * kMxRows + 4 * i + r4, M - 1));
+    typedef uint32_t words __attribute__((ext_vector_type(F32 ? 8 : 4)));
+#pragma unroll
+    for (int h0 = 0; h0 < 2; h0 += AT_ONCE) {
+        words w[AT_ONCE][8];
+#pragma unroll
+        for (int half = 0; half < AT_ONCE; ++half) {
+            const int k = step * kMxStep + 128 * (h0 + half) + 32 * blk + 8 * piece;
+            const long long col = k < K ? x.column<E>(k) : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int n = tile * kMxRows + 4 * i + r4 < M ? K - k : 0;
+                words v = 0;
+                if (n >= 8) {
+                    typedef uint32_t chunk __attribute__((ext_vector_type(4), aligned(2)));       // rows start anywhere
+#pragma unroll
+                    for (int j = 0; j < WORDS / 4; ++j) {
+                        const chunk c = __builtin_nontemporal_load(reinterpret_cast<const chunk*>(row[i] + col) + j);
+                        v[4 * j] = c.x; v[4 * j + 1] = c.y; v[4 * j + 2] = c.z; v[4 * j + 3] = c.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 7; ++j)
+                        if (j < n) {
+                            if (F32) v[j & 7] = reinterpret_cast<const uint32_t*>(row[i] + col)[j];
+                            else     v[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(row[i] + col)[j] << (16 * (j & 1));
+                        }
+                }
+                w[half][i] = v;
+            }
+        }
+#pragma unroll
+        for (int half = 0; half < AT_ONCE; ++half)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const words v = w[half][i];
+                uint32_t top = 0;
+#pragma unroll
+                for (int j = 0; j < WORDS; ++j) {
+                    const uint32_t lo = F32 ? v[j] & 0x7FFFFFFFu : v[j] << 16 & 0x7FFF0000u, hi = F32 ? 0u : v[j] & 0x7FFF0000u;
+                    top = lo > top ? lo : top;
+                    top = hi > top ? hi : top;
+                }
+                auto other = [&](auto ctrl) __attribute__((always_inline)) {
+                    const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, decltype(ctrl)::value, 0xf, 0xf, false);
+                    top = o > top ? o : top;
+                };
+                other(Count<0xB1>{});
+                other(Count<0x4E>{});
+                const BlockScale s = block_scale(top);
+                uint32_t r = 0;
+                if constexpr (F32) {
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(v[0]), __uint_as_float(v[1]), s.value, 0);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(v[2]), __uint_as_float(v[3]), s.value, 1);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(v[4]), __uint_as_float(v[5]), s.value, 2);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, __uint_as_float(v[6]), __uint_as_float(v[7]), s.value, 3);
+                } else {
+                    const uint32_t w0 = v[0], w1 = v[1], w2 = v[2], w3 = v[3];       // a cast of an element itself takes the first one
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w0), s.value, 0);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w1), s.value, 1);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w2), s.value, 2);
+                    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(bf16x2, w3), s.value, 3);
+                }
+                const int b4 = 4 * (h0 + half) + blk, n = 4 * i + r4;                // block of the step: quarter b4 / 2, half b4 % 2
+                *reinterpret_cast<uint32_t*>(mine + b4 * GROUP + 16 * n + 4 * piece) = r;
+                if (piece == 0) mine[CODES + (32 * (b4 & 1) + n) * 4 + (b4 >> 1)] = (uint8_t)s.byte;
+            }
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        codes[((long long)wave * 4 + q) * 64 + lane] = *reinterpret_cast<const uint4*>(mine + (2 * q + (lane >> 5)) * GROUP + 16 * (lane & 31));
+    scales[(long long)wave * 64 + lane] = *reinterpret_cast<const uint32_t*>(mine + CODES + 4 * lane);
 }
 
 // Eight elements a lane, so that its 32 lanes store a row's 256 in a run; a wave two rows at a time, whose codes lie about the step's 4 KB.
@@ -226,7 +323,9 @@ __global__ __launch_bounds__(64 * KW) void mx4_matmul_kernel(Packed a, Packed b,
 }
 
 // ---- launches -----------------------------------------------------------------------------------
-// Fewer than 1024 tiles' steps: a quarter of a step a wave, and four times as many waves.  851 x 1536 in bf16 7.2 -> 3.7 us.
+// Fewer than 1024 tiles' steps: a quarter of a step a wave, and four times as many waves.  851 x 1536 in bf16 7.2 -> 3.7 us.  More than the Infinity
+// Cache's 256 MB: past the caches.  75600 x 5120 in bf16 184 -> 155 us (6.3 TB/s), from heads 182 -> 161, and the product behind it 875 -> 890;
+// 32760 x 1536, which the cache holds, 20.4 us (6.2 TB/s), past the caches 22.4.
 int launch_mx4_quantize(const fps_view& v, void* packed, hipStream_t st) {
     const Matrix x(v);
     const Packed p(packed, x.all_rows(), x.all_cols());
@@ -237,8 +336,11 @@ int launch_mx4_quantize(const fps_view& v, void* packed, hipStream_t st) {
         mx4_quantize_kernel<decltype(f32)::value, QS><<<(waves + 3) / 4, 256, 0, st>>>(x, (uint4*)p.codes, (uint32_t*)p.scales, p.steps, waves);
     };
     auto typed = [&](auto f32) {
-        if (at < 1024) launch(f32, Count<1>{});
-        else           launch(f32, Count<4>{});
+        constexpr bool F32 = decltype(f32)::value;
+        if ((long long)x.all_rows() * x.all_cols() * (F32 ? 4 : 2) > (256LL << 20))
+            mx4_quantize_rows_kernel<F32><<<(at + 3) / 4, 256, 0, st>>>(x, (uint4*)p.codes, (uint32_t*)p.scales, p.steps, at);
+        else if (at < 1024) launch(f32, Count<1>{});
+        else                launch(f32, Count<4>{});
     };
     if (v.dt == FPS_OUT_F32) typed(std::true_type{});
     else                     typed(std::false_type{});

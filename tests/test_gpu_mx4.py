@@ -66,6 +66,29 @@ def test_values_of_views(B, heads, tokens, cols, dt):
     assert same(back.transpose(1, 2).reshape(m.shape), op.mx4_values(m))
 
 
+@pytest.mark.parametrize("dt,rows,K", [(BF16, 26400, 5137), (F32, 14000, 5003), (BF16, 1, 140000001), (BF16, 2200000, 65)])
+def test_values_beyond_the_caches(dt, rows, K):
+    """More than 256 MB of rows, which are read past the caches; with infinities and NaN in them."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    x = rows_of(gen, rows, K, dt, spread=3.0)
+    x[rows // 2, K // 3], x[0, K - 1], x[rows - 1, 0] = float("nan"), float("inf"), float("-inf")
+    packed = fps.mx4_quantize(x)
+    assert same(fps.mx4_dequantize(packed, rows, K), op.mx4_values(x))
+    part = min(rows, 4096)                                   # the same codes as of fewer rows
+    assert torch.equal(fps.mx4_quantize(x[:part])[:fps.mx4_bytes(part, K) // 17 * 16], packed[:fps.mx4_bytes(part, K) // 17 * 16])
+    if rows % 2 == 0:
+        half = x.view(2, rows // 2, K)                       # in two parts of rows
+        assert torch.equal(fps.mx4_quantize(half), packed)
+
+
+def test_views_beyond_the_caches():
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    x = torch.randn(2, 9, 60000, 128, generator=gen, device=DEV).to(BF16)
+    m = x.transpose(1, 2).reshape(120000, 9 * 128).contiguous()
+    assert torch.equal(fps.mx4_quantize(x), fps.mx4_quantize(m))
+    assert torch.equal(fps.mx4_quantize(m[:, :1000]), fps.mx4_quantize(m[:, :1000].contiguous()))
+
+
 def test_every_bf16_value_and_the_scales_ends():
     """Blocks that hold one value beside a largest one of every exponent; blocks of zeros, of subnormal numbers, of the largest
     number; infinities and NaN make a block NaN and no other."""
@@ -79,6 +102,9 @@ def test_every_bf16_value_and_the_scales_ends():
         assert same(fps.mx4_dequantize(packed, 65536, 64, out_dtype=F32), want)
         assert same(fps.mx4_dequantize(fps.mx4_quantize(x.float()), 65536, 64, out_dtype=F32), want)
         assert bool((want[:, 32] == 1).all())
+    wide = x.repeat(1, 33)                                   # read past the caches
+    assert same(fps.mx4_dequantize(fps.mx4_quantize(wide), 65536, 64 * 33, out_dtype=F32)[:, -64:], want)
+    assert same(fps.mx4_dequantize(fps.mx4_quantize(wide.float()), 65536, 64 * 33, out_dtype=F32)[:, -64:], want)
 
 
 def test_every_quotient_near_a_tie_in_fp32():
