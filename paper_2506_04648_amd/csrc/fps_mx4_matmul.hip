@@ -3,7 +3,11 @@
 // A workgroup of four waves, one on each SIMD of a CU, takes 256 x 256 elements of the result, a wave 128 x 128 of them in 256
 // accumulation registers; it stays on its CU and goes from tile to tile.  Half a step of both operands, 128 columns in 32 KB,
 // is a slot of a ring of four in the LDS; a slot is filled again as soon as it is read, three of them before it is needed, across the
-// end of a tile as well.
+// end of a tile as well.  Of results with fewer tiles, 128 x 128 elements in the same manner, two workgroups a CU.
+//
+// Bound by the matrix instructions and by the power they take: alone they reach 6.0 to 6.8 PFLOP/s (10 at the nominal clock).  75600 x 5120 x 5120
+// 887 us, 4.5 PFLOP/s; 16384 x 16384 x 16384 1.77 ms, 5.0.  (A whole step copied ahead instead of the
+// ring, 16384^3 1.93 ms; the result stored between the tiles instead of among the next one's multiplications, 32760 x 1536 x 4608 166 us instead of 143.)
 #include "fps_mx4.h"
 
 namespace fps {
@@ -64,9 +68,10 @@ __device__ __forceinline__ Place place_of(const TileMap& t, int i) {
     return Place{8 * g + rem - col * down, col};
 }
 
-template <int WT, bool F32, bool HIDDEN>
+template <int WT, bool F32, bool HIDDEN, bool PAST>
 __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mx4_large_kernel(Packed a, Packed b, const float* __restrict__ bias, Matrix y, TileMap map) {
     static_assert(!HIDDEN || (WT == 4 && !F32), "a result on its way among the next tile's multiplications is in bf16");
+    static_assert(!PAST || HIDDEN, "only those stores pass the caches");
     using L = Tile<WT, F32>;
     constexpr int QUARTER = WT * WT, COPIES = 2 * WT;        // multiplications of 64 columns; copies of half a step, without scales
     __shared__ __attribute__((aligned(1024))) uint8_t lds[L::BYTES];
@@ -202,7 +207,7 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mx4_large_kernel(Packed 
         const int down = 32 * (k >> 1) + 8 * t;
         const uint32_t outside = (uint32_t)((done_rows - 1 - down - at.row) >> 31);
         typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-        __builtin_amdgcn_raw_buffer_store_b128(u32x4{chunk[t & 1].x, chunk[t & 1].y, chunk[t & 1].z, chunk[t & 1].w}, done, done_at[k & 1] | outside, down * stride_r, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{chunk[t & 1].x, chunk[t & 1].y, chunk[t & 1].z, chunk[t & 1].w}, done, done_at[k & 1] | outside, down * stride_r, PAST ? 2 : 0);       // 2: past the caches
     };
     // What follows multiplication n of 64 of a tile's first step: piece n / 8 is written, and its four chunks are read and, two
     // multiplications later, stored, two at a time (there are no registers for more)
@@ -381,12 +386,16 @@ static int launch_tiles(const void* pa, const void* pb, int K, const float* bias
         // batch whose elements do not follow each other is written between the tiles
         const bool chunks = y.all_cols() % 8 == 0 && (y.stride_h | y.stride_r) % 16 == 0;
         const bool near = y.stride_r < (1 << 22) && 128 * y.stride_r + (y.heads - 1) * y.stride_h + 2LL * y.cols < 0xFFFFFFF0LL;
-        if (v.dt == FPS_OUT_F32)             mx4_large_kernel<4, true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-        else if (y.B == 1 && chunks && near) mx4_large_kernel<4, false, true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-        else                                 mx4_large_kernel<4, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        // and past the caches, which keep the operands, where the result is more than the Infinity Cache's 256 MB: 75600 x 5120 x 5120 909 -> 887 us,
+        // 32760 x 1536 x 4608 148 -> 140; of less, which the cache holds for what reads it next, 8192 x 5120 x 5120 117, 116
+        const bool past = 2LL * y.all_rows() * y.all_cols() > (256LL << 20);
+        if (v.dt == FPS_OUT_F32)               mx4_large_kernel<4, true, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else if (y.B > 1 || !chunks || !near)  mx4_large_kernel<4, false, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else if (past)                         mx4_large_kernel<4, false, true, true><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else                                   mx4_large_kernel<4, false, true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
     } else {
-        if (v.dt == FPS_OUT_F32) mx4_large_kernel<2, true, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
-        else                     mx4_large_kernel<2, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        if (v.dt == FPS_OUT_F32) mx4_large_kernel<2, true, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
+        else                     mx4_large_kernel<2, false, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
     }
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");

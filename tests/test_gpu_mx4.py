@@ -125,7 +125,7 @@ SIZES = [(1, 1, 1), (1, 64, 64), (1, 5120, 640), (2, 33, 100), (7, 160, 33), (32
 # From 112 tiles of 128 x 128 on they are what is multiplied, one step of K or more, the last tile cut; tiles of 256 where they fill the CUs
 # better, up to several of them one after the other
 SIZES += [(33, 300, 15000), (1400, 1100, 1501), (1500, 64, 1496), (15000, 200, 1), (5000, 257, 4100)]
-SIZES += [(7000, 64, 2104), (7001, 300, 2103), (8200, 520, 4104), (6921, 1792, 2048), (12000, 256, 5128)]
+SIZES += [(7000, 64, 2104), (7001, 300, 2103), (8200, 520, 4104), (6921, 1792, 2048), (12000, 256, 5128), (26333, 64, 5128)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
