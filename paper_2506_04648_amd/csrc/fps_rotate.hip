@@ -13,6 +13,7 @@ namespace fps {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
@@ -62,13 +63,14 @@ template <bool HALVES, typename F> __device__ __forceinline__ Pairs pairs_of(F&&
 
 // an input row's 16 channels, BY4 = F32
 template <bool F32> struct Chunks { uint32_t __attribute__((ext_vector_type(F32 ? 16 : 8))) w; };
-template <bool F32>
+template <bool F32, bool PAST = false>                       // PAST: what is read does not stay in the caches
 __device__ __forceinline__ Chunks<F32> load_row(const char* row, int u) {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     Chunks<F32> c;
 #pragma unroll
     for (int i = 0; i < (F32 ? 4 : 2); ++i) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(row + 128 * i + 16 * u);
+        const u32x4* at = reinterpret_cast<const u32x4*>(row + 128 * i + 16 * u);
+        const u32x4 v = PAST ? __builtin_nontemporal_load(at) : *at;
         c.w[4 * i] = v.x; c.w[4 * i + 1] = v.y; c.w[4 * i + 2] = v.z; c.w[4 * i + 3] = v.w;
     }
     return c;
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
     Chunks<IN32> c[HC];
 #pragma unroll
     for (int i = 0; i < HC; ++i)
-        if (h0 + i < heads) c[i] = load_row<IN32>(x.at(b, h0 + i, n), u);
+        if (h0 + i < heads) c[i] = load_row<IN32, PAST>(x.at(b, h0 + i, n), u);
     const Turn turn = load_turn<IN32, HALVES>(k, b, n, u);
 #pragma unroll
     for (int i = 0; i < HC; ++i) {
@@ -220,7 +222,7 @@ constexpr int kWhole = -1, kStaged = 1024;
 // which the next one's rows are on their way while one is worked on.
 constexpr int kManyHeads = 4;
 struct Units { int heads, parts, count; uint32_t rc; };      // heads of a workgroup, workgroups for all heads; groups (blocks) of a head
-template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED, bool MANY>
+template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED, bool MANY, bool PAST>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
                                                                            float* __restrict__ scales, int role, Geom g,
                                                                            int heads, Units units) {
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         token[i] = real_token(org.box, slot < org.box.n ? slot : org.box.n > 0 ? org.box.n - 1 : 0);
         from[i] = x.at(b, head0, n0) + ((token[i].t * g.H + token[i].h) * g.W + token[i].w) * x.r;
         ahead[i].w = 0;
-        if (slot < org.box.n) ahead[i] = load_row<IN32>(from[i], u);
+        if (slot < org.box.n) ahead[i] = load_row<IN32, PAST>(from[i], u);
     }
     // the group's entries: its planes' and rows' are runs of the table, its columns' each a run and as many (1, 0) as there are pairs left
     const int t0 = quotient(n0, g.H * g.W, k.rc_plane), h0 = quotient(n0 - t0 * (g.H * g.W), g.W, k.rc_row), w0 = n0 - (t0 * g.H + h0) * g.W;
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
             now[i] = ahead[i];
             if (MANY && head < last_head) {
                 from[i] += x.h;
-                if (org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i < org.box.n) ahead[i] = load_row<IN32>(from[i], u);
+                if (org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i < org.box.n) ahead[i] = load_row<IN32, PAST>(from[i], u);
             }
         }
         Pairs y[U];                                              // without the norm's factor r of the row
@@ -376,7 +378,8 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 const int c = channel_of<IN32>(u, 4 * m);
                 char* at = dst + 16 * chunk(c >> 4) + (c & 15);
                 if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
-                else      *reinterpret_cast<uint2*>(at) = make_uint2(o[m], o[(m + 1) & 3]);
+                else if (PAST) __builtin_nontemporal_store(u32x2{o[m], o[(m + 1) & 3]}, reinterpret_cast<u32x2*>(at));
+                else           *reinterpret_cast<u32x2*>(at) = u32x2{o[m], o[(m + 1) & 3]};
             }
         }
     }
@@ -409,8 +412,8 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
 #pragma unroll
         for (int i = 0; i < HC; ++i)
             if (h0 + i < heads) {
-                cx[i] = load_row<F32>(x.at(b, h0 + i, n), u);
-                cy[i] = load_row<F32>(dy.at(b, h0 + i, n), u);
+                cx[i] = load_row<F32, PAST>(x.at(b, h0 + i, n), u);
+                cy[i] = load_row<F32, PAST>(dy.at(b, h0 + i, n), u);
             }
         const Turn turn = load_turn<F32, HALVES>(k, b, n, u);
         Pairs w = load_weight<F32, HALVES>(k, h0, u);
@@ -580,11 +583,12 @@ static Turning turning_of(const Geom& g, const fps_norm* norm, const fps_rotatio
     k.rc_row = reciprocal(g.W);
     return k;
 }
-// Input and output together beyond the Infinity Cache's 256 MB: the output does not push out what is there.  720p 303 -> 291 us, its gradient
-// 462 -> 450; of 480p, which the cache holds for what reads it next, 43.6 -> 39.4.
+// Input and output together beyond the Infinity Cache's 256 MB: the output does not push out what is there.  And what is read once
+// goes past it too.  720p 303 -> 291 -> 278 us, its gradient 468 -> 458 by the latter; 480p, which the cache holds for what reads it next, 31.6 us, 37.4 past it.
+constexpr long long kCaches = 256LL << 20;
 static bool beyond_caches(const fps_view& x, const fps_view& y) {
     const long long n = (long long)x.B * x.heads * x.rows * kHeadDim;
-    return n * ((x.dt == FPS_OUT_F32 ? 4 : 2) + (y.dt == FPS_OUT_F32 ? 4 : 2)) > (256LL << 20);
+    return n * ((x.dt == FPS_OUT_F32 ? 4 : 2) + (y.dt == FPS_OUT_F32 ? 4 : 2)) > kCaches;
 }
 static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_PAIRS_HALVES; }
 
@@ -622,7 +626,7 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate launch");
 }
 
-template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY>
+template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY, bool PAST>
 static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                            hipStream_t st) {
     // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
@@ -636,23 +640,23 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
     const Launch blocks = of_head(g.M * g.KB, MANY);
     const int groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY, PAST><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         return;
     }
     auto whole = [&](auto nb) {
         constexpr int NB = decltype(nb)::value, T = TH * NB > 1024 ? TH / 2 : TH;
         constexpr bool many = MANY && T == TH;               // twice the rows a lane: no registers for the next head's
         const Launch l = of_head(g.M * g.NS, many);
-        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
+        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many, many && PAST><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
     };
     if (g.KBS == 1)      whole(Count<1>{});
     else if (g.KBS == 2) whole(Count<2>{});
     else if (g.KBS == 3) whole(Count<3>{});
     else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
         if (g.KBS == 4) return whole(Count<4>{});            // 512 tokens, 1024 threads: one pass instead of two and three launches less
-        clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);     // x is read twice: by way of the caches
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY, false><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY, false><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         amax_to_scale_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
 }
@@ -663,16 +667,20 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
     const bool staged = (long long)g.Qt * k.ct + (long long)g.Qh * k.ch + (long long)g.Qw * (64 - k.ct - k.ch) <= kStaged;
     // Several heads a workgroup where there are 1024 blocks of 128 slots or more (bf16, one weight for all: the staged turns hold
     // it; fp32 rows leave no registers).  us with one head, with four: 480p of 12 heads 38.9, 32.7 (BF16 48.8, 43.8), 720p of 40 heads 247,
-    // 226 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12 heads, 540 blocks of 128, 9.6, 11.1
+    // 227 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12 heads, 540 blocks of 128, 9.6, 11.1
     const bool many = staged && x.heads > 1 && !k.weight_head && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
-    auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn) {
-        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value>(
+    // past the caches: 720p of 40 heads 228 -> 210 us (BF16 306 -> 296); 480p of 12, which they hold, 33.4, 36.3
+    const bool past = (long long)x.B * x.heads * x.rows * kHeadDim * (prec == FPS_PREC_FP8 ? 3 : 4) > kCaches;
+    auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn, auto pa) {
+        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value, decltype(pa)::value>(
             g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
     };
     with(g.BS == 128, [&](auto big) { with(halves(rot), [&](auto hv) {
-        if (x.dt == FPS_OUT_F32) with(staged, [&](auto sg) { launch(big, std::true_type{}, hv, sg, std::false_type{}); });
-        else if (many)           launch(big, std::false_type{}, hv, std::true_type{}, std::true_type{});
-        else                     with(staged, [&](auto sg) { launch(big, std::false_type{}, hv, sg, std::false_type{}); });
+        const std::true_type yes;
+        const std::false_type no;
+        if (x.dt == FPS_OUT_F32) with(staged, [&](auto sg) { launch(big, yes, hv, sg, no, no); });
+        else if (many)           with(past, [&](auto pa) { launch(big, no, hv, yes, yes, pa); });
+        else                     with(staged, [&](auto sg) { launch(big, no, hv, sg, no, no); });
     }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");

@@ -166,6 +166,8 @@ OPERANDS = [
     dict(grid=(9, 60, 70), tile=(3, 4, 4), heads=9, qtile=(1, 4, 4)),                          # blocks of 32
     dict(grid=(9, 60, 70), tile=(8, 8, 8), heads=5, layout="fused"),                           # four blocks: one head
     dict(grid=(9, 60, 70), tile=(1, 8, 16), heads=5, B=2, layout="fused", weight="per_head"),
+    dict(grid=(16, 61, 67), tile=(1, 8, 16), heads=11, layout="fused", halves=True),           # beyond 256 MB in and out together
+    dict(grid=(16, 61, 67), tile=(4, 16, 16), heads=11),
 ]
 
 
