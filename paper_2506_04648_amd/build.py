@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
@@ -23,7 +24,7 @@ def build_lib(verbose: bool = False) -> str:
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              # no NaN ever enters the attention (inputs are finite, masked scores are -inf, never inf-inf): lets fmax/fmin
              # compile without the canonicalising v_max(x,x) in front of every operand; the other kernels and the host compare bits
-             "-fno-honor-nans", "-parallel-jobs=8"] + os.environ.get("FPS_EXTRA_HIPCC_FLAGS", "").split()
+             "-fno-honor-nans"] + os.environ.get("FPS_EXTRA_HIPCC_FLAGS", "").split()
     # MFMA results stay in architectural VGPRs: the softmax VALU code reads them directly instead of through
     # v_accvgpr moves
     vgpr_form = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
@@ -36,10 +37,12 @@ def build_lib(verbose: bool = False) -> str:
         if res.returncode != 0:
             raise RuntimeError("hipcc failed building libfps.so")
 
-    with tempfile.TemporaryDirectory() as tmp:
-        objects = [os.path.join(tmp, s + ".o") for s in AGPR_SOURCES]
-        for source, obj in zip(AGPR_SOURCES, objects):
-            run([hipcc, *flags, "-c", os.path.join(CSRC, source), "-o", obj])
-        run([hipcc, *flags, *vgpr_form, "-shared", "-o", OUT] + [os.path.join(CSRC, s) for s in SOURCES if s not in AGPR_SOURCES]
-            + objects)
+    # each source to an object of its own, which the link takes alone: behind a source hipcc takes an object for one as well
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(8) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        jobs = [pool.submit(run, [hipcc, *flags, *([] if s in AGPR_SOURCES else vgpr_form), "-c", os.path.join(CSRC, s), "-o", o])
+                for s, o in zip(SOURCES, objects)]
+        for job in jobs:
+            job.result()
+        run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT] + objects)
     return OUT

@@ -203,3 +203,19 @@ def test_the_binding_refuses_products():
             fps.mx4_linear(x, w, 9, out=out)
     three = torch.zeros(2, 5, 70)[:, 1:]
     assert [getattr(fps._matrix(three, "x"), n) for n in ("B", "heads", "rows", "cols", "stride_b", "stride_r")] == [2, 1, 4, 70, 350, 70]
+
+
+def test_the_build_links_objects_alone(tmp_path, monkeypatch):
+    """hipcc takes an object that follows a source for a source: each source is compiled by itself, once, and the link has objects only."""
+    from paper_2506_04648_amd import build
+    log, stub = tmp_path / "log", tmp_path / "hipcc"
+    stub.write_text(f'#!/bin/sh\necho "$@" >> {log}\n')
+    stub.chmod(0o755)
+    monkeypatch.setenv("HIPCC", str(stub))
+    monkeypatch.setattr(build, "OUT", str(tmp_path / "lib.so"))
+    build.build_lib()
+    commands = [line.split() for line in log.read_text().splitlines()]
+    sources = sorted(a.rsplit("/", 1)[-1] for c in commands[:-1] for a in c if a.endswith((".hip", ".cpp")))
+    assert sources == sorted(build.SOURCES) and all(sum(a.endswith((".hip", ".cpp")) for a in c) == 1 for c in commands[:-1])
+    assert "-shared" in commands[-1] and not any(a.endswith((".hip", ".cpp")) for a in commands[-1])
+    assert sum(a.endswith(".o") for a in commands[-1]) == len(build.SOURCES)
