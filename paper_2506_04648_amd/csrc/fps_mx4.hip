@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_rows_kernel(Matrix x, uint4*
                 if (piece == 0) mine[CODES + (32 * (b4 & 1) + n) * 4 + (b4 >> 1)] = (uint8_t)s.byte;
             }
     }
-    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");                           // the wave's reads stay behind its writes
 #pragma unroll
     for (int q = 0; q < 4; ++q)
         codes[((long long)wave * 4 + q) * 64 + lane] = *reinterpret_cast<const uint4*>(mine + (2 * q + (lane >> 5)) * GROUP + 16 * (lane & 31));

@@ -53,7 +53,7 @@ def test_values(rows, K, dt):
 
 
 @pytest.mark.parametrize("dt", [BF16, F32])
-@pytest.mark.parametrize("B,heads,tokens,cols", [(1, 3, 7, 128), (2, 2, 33, 128), (2, 5, 11, 32), (3, 1, 9, 40)])
+@pytest.mark.parametrize("B,heads,tokens,cols", [(1, 3, 7, 128), (2, 2, 33, 128), (2, 5, 11, 32), (3, 1, 9, 40), (3, 2, 1, 128), (40, 1, 1, 33)])
 def test_values_of_views(B, heads, tokens, cols, dt):
     say("views", B, heads, tokens, cols, dt)
     gen = torch.Generator(device=DEV).manual_seed(tokens)
@@ -148,7 +148,7 @@ def test_product(M, K, N):
         assert torch.equal(fps.mx4_linear(x.float(), b, N, bias=add, out_dtype=F32), y)
 
 
-@pytest.mark.parametrize("B,heads_in,heads_out,tokens", [(1, 2, 3, 45), (2, 4, 5, 31), (3, 1, 2, 200), (1, 5, 12, 700), (2, 2, 12, 700), (1, 1, 17, 7000),
+@pytest.mark.parametrize("B,heads_in,heads_out,tokens", [(1, 2, 3, 45), (2, 4, 5, 31), (3, 1, 2, 200), (1, 5, 12, 700), (2, 2, 12, 700), (1, 1, 17, 7000), (4, 2, 3, 1), (1500, 1, 12, 1),
                                                           (2, 3, 16, 3500)])
 def test_product_between_the_attentions_layouts(B, heads_in, heads_out, tokens):
     say("layouts", B, heads_in, heads_out, tokens)
