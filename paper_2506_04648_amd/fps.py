@@ -79,6 +79,7 @@ class FpsError(RuntimeError):
 
 _lib = None
 _torch = None                                  # the module, once a device entry point has needed it
+_codes = {}                                    # of torch's types, from then on
 
 
 def _import_torch():
@@ -174,11 +175,11 @@ def make_step_cfg(step, num_steps, alpha1, alpha2, regimes) -> StepCfg:
     return cfg
 
 
-def _stream():
+def _stream(device=None):
     # the handle alone: building a Stream object around it takes 3 us, as long as the launch itself
     torch = _torch or _import_torch()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not in torch's documented interface
-    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+    return raw(torch.cuda.current_device() if device is None else device) if raw else torch.cuda.current_stream().cuda_stream
 
 
 def _ptr(t):
@@ -376,16 +377,18 @@ def attn_fwd(shape: Shape, window, prec, q, k, v, sq=None, sk=None, sv=None, vsc
 
 # ---- before and after the attention -------------------------------------------------------------
 def _here(*tensors):
-    """Every tensor (None: left out) is on the current device, whose stream the call goes to."""
+    """Every tensor (None: left out) is on the current device; returns its stream, which the call goes to."""
     current = None
     for t in tensors:
         if t is None:
             continue
         device = t.get_device()                            # -1 on the host
-        if current is None and device >= 0:
-            current = (_torch or _import_torch()).cuda.current_device()
-        if device < 0 or device != current:
-            raise ValueError(f"a tensor on {t.device}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
+        if device != current:
+            if current is None and device >= 0:
+                current = (_torch or _import_torch()).cuda.current_device()
+            if device != current:
+                raise ValueError(f"a tensor on {t.device}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
+    return _stream(current)
 
 
 def _whole(t, dtype, numel, name):
@@ -394,12 +397,13 @@ def _whole(t, dtype, numel, name):
 
 
 def _dtype_code(t):
-    torch = _torch or _import_torch()
-    if t.dtype == torch.bfloat16:
-        return OUT_BF16
-    if t.dtype == torch.float32:
-        return OUT_F32
-    raise ValueError(f"{t.dtype} instead of bfloat16 or float32")
+    if not _codes:
+        torch = _torch or _import_torch()
+        _codes.update({torch.bfloat16: OUT_BF16, torch.float32: OUT_F32})
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{t.dtype} instead of bfloat16 or float32")
+    return code
 
 
 def _view(t, name) -> View:
@@ -481,8 +485,8 @@ def norm_rotate(shape: Shape, x, norm: Norm = None, rotation: Rotation = None, o
     if out is None:
         out = torch.empty((shape.B, shape.heads, shape.T, shape.H, shape.W, shape.head_dim), dtype=out_dtype or x.dtype,
                           device=x.device)
-    _here(x, out, weight, table)
-    _check(lib().fps_norm_rotate(shape, _view(x, "x"), norm, rotation, _view(out, "out"), _stream()))
+    stream = _here(x, out, weight, table)
+    _check(lib().fps_norm_rotate(shape, _view(x, "x"), norm, rotation, _view(out, "out"), stream))
     return out
 
 
@@ -497,11 +501,11 @@ def norm_rotate_operand(shape: Shape, x, role, prec=PREC_FP8, norm: Norm = None,
         scales = None
     elif scales is None:
         scales = torch.empty((shape.B, shape.heads, num_groups(shape)), dtype=torch.float32, device=x.device)
-    _here(x, out, scales, weight, table)
+    stream = _here(x, out, scales, weight, table)
     _whole(out, torch.uint8, packed_bytes(shape, prec), "out")
     if fp8:
         _whole(scales, torch.float32, shape.B * shape.heads * num_groups(shape), "scales")
-    _check(lib().fps_norm_rotate_operand(shape, _view(x, "x"), norm, rotation, role, prec, out.data_ptr(), _ptr(scales), _stream()))
+    _check(lib().fps_norm_rotate_operand(shape, _view(x, "x"), norm, rotation, role, prec, out.data_ptr(), _ptr(scales), stream))
     return out, scales
 
 
@@ -528,10 +532,10 @@ def norm_rotate_bwd(shape: Shape, x, dy, norm: Norm = None, rotation: Rotation =
         _whole(dweight, torch.float32, weight.numel(), "dweight")
         if workspace is None:
             workspace = torch.empty(norm_rotate_bwd_bytes(shape, norm), dtype=torch.uint8, device=x.device)
-    _here(x, dy, dx, dweight, workspace, weight, table)
+    stream = _here(x, dy, dx, dweight, workspace, weight, table)
     _check(lib().fps_norm_rotate_bwd(shape, _view(x, "x"), norm, rotation, _view(dy, "dy"), _view(dx, "dx"), _ptr(dweight),
                                      _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     _stream()))
+                                     stream))
     return dx, dweight
 
 
@@ -541,26 +545,31 @@ def dequantize(shape: Shape, xq, scales, role, vscale=VSCALE_TILE, out=None, out
     dims = (shape.B, shape.heads, shape.T, shape.H, shape.W, shape.head_dim)
     if out is None:
         out = torch.empty(dims, dtype=out_dtype or torch.bfloat16, device=xq.device)
-    _here(xq, scales, out)
+    stream = _here(xq, scales, out)
     _whole(xq, torch.uint8, packed_bytes(shape, PREC_FP8), "xq")
     _whole(out, out.dtype, shape.B * shape.heads * shape.T * shape.H * shape.W * shape.head_dim, "out")
     n = shape.head_dim if role == ROLE_V and vscale == VSCALE_CHANNEL else num_groups(shape)
     _whole(scales, torch.float32, shape.B * shape.heads * n, "scales")
-    _check(lib().fps_dequantize(shape, xq.data_ptr(), scales.data_ptr(), role, vscale, _dtype_code(out), out.data_ptr(), _stream()))
+    _check(lib().fps_dequantize(shape, xq.data_ptr(), scales.data_ptr(), role, vscale, _dtype_code(out), out.data_ptr(), stream))
     return out
 
 
-def _matrix(t, name) -> View:
+def _matrix(t, name):
     """A matrix [rows, cols], several [B, rows, cols], or a tensor [B, heads, tokens.., cols] whose matrix has B * tokens rows of
-    heads * cols; columns of a row (of a head) are contiguous."""
-    if t.dim() >= 4:
-        return _view(t, name)
-    if t.dim() < 2:
-        raise ValueError(f"{name} must have rows and columns, not {tuple(t.shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    heads * cols; columns of a row (of a head) are contiguous.  Returns its View, rows and columns."""
+    size, stride = t.shape, t.stride()
+    n = len(size)
+    if n >= 4:
+        v = _view(t, name)
+        return v, v.B * v.rows, v.heads * v.cols
+    if n < 2:
+        raise ValueError(f"{name} must have rows and columns, not {tuple(size)}")
+    rows, cols = size[-2], size[-1]
+    if stride[-1] != 1 and cols > 1:
         raise ValueError(f"{name}: the columns must be contiguous")
-    B, stride_b = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
-    return View(t.data_ptr(), _dtype_code(t), B, 1, t.shape[-2], t.shape[-1], stride_b, 0, t.stride(-2))
+    if n == 2:
+        return View(t.data_ptr(), _dtype_code(t), 1, 1, rows, cols, 0, 0, stride[0]), rows, cols
+    return View(t.data_ptr(), _dtype_code(t), size[0], 1, rows, cols, stride[0], 0, stride[1]), size[0] * rows, cols
 
 
 def mx4_bytes(rows, cols) -> int:
@@ -581,13 +590,13 @@ def mx4_linear_bytes(rows, cols) -> int:
 def mx4_quantize(x, out=None):
     """bf16 or fp32 rows (see _matrix) -> packed blocks of 32 E2M1 codes with a power of two each."""
     torch = _torch or _import_torch()
-    v = _matrix(x, "x")
-    n = mx4_bytes(v.B * v.rows, v.heads * v.cols)
+    v, rows, cols = _matrix(x, "x")
+    n = mx4_bytes(rows, cols)
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=x.device)
-    _here(x, out)
+    stream = _here(x, out)
     _whole(out, torch.uint8, n, "out")
-    _check(lib().fps_mx4_quantize(v, out.data_ptr(), _stream()))
+    _check(lib().fps_mx4_quantize(v, out.data_ptr(), stream))
     return out
 
 
@@ -596,21 +605,21 @@ def mx4_dequantize(packed, rows, cols, out=None, out_dtype=None):
     torch = _torch or _import_torch()
     if out is None:
         out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=packed.device)
-    _here(packed, out)
-    v = _matrix(out, "out")
-    if (v.B * v.rows, v.heads * v.cols) != (rows, cols):
+    stream = _here(packed, out)
+    v, *size = _matrix(out, "out")
+    if size != [rows, cols]:
         raise ValueError(f"out {tuple(out.shape)} is not a matrix of {rows} x {cols}")
     _whole(packed, torch.uint8, mx4_bytes(rows, cols), "packed")
-    _check(lib().fps_mx4_dequantize(packed.data_ptr(), v, _stream()))
+    _check(lib().fps_mx4_dequantize(packed.data_ptr(), v, stream))
     return out
 
 
-def _product_out(out, out_dtype, rows, cols, device):
+def _product_out(out, out_dtype, rows, cols, like):
     torch = _torch or _import_torch()
     if out is None:
-        out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=device)
-    v = _matrix(out, "out")
-    if (v.B * v.rows, v.heads * v.cols) != (rows, cols):
+        out = torch.empty((rows, cols), dtype=out_dtype or torch.bfloat16, device=like.device)
+    v, r, c = _matrix(out, "out")
+    if r != rows or c != cols:
         raise ValueError(f"out {tuple(out.shape)} is not a matrix of {rows} x {cols}")
     return out, v
 
@@ -618,28 +627,27 @@ def _product_out(out, out_dtype, rows, cols, device):
 def mx4_matmul(a, b, m, n, k, bias=None, out=None, out_dtype=None):
     """a b^T + bias of packed matrices a [m, k] and b [n, k]; bias: fp32 [n]."""
     torch = _torch or _import_torch()
-    out, v = _product_out(out, out_dtype, m, n, a.device)
-    _here(a, b, bias, out)
+    out, v = _product_out(out, out_dtype, m, n, a)
+    stream = _here(a, b, bias, out)
     _whole(a, torch.uint8, mx4_bytes(m, k), "a")
     _whole(b, torch.uint8, mx4_bytes(n, k), "b")
     if bias is not None:
         _whole(bias, torch.float32, n, "bias")
-    _check(lib().fps_mx4_matmul(k, a.data_ptr(), b.data_ptr(), _ptr(bias), v, _stream()))
+    _check(lib().fps_mx4_matmul(k, a.data_ptr(), b.data_ptr(), _ptr(bias), v, stream))
     return out
 
 
 def mx4_linear(x, w, n, bias=None, out=None, out_dtype=None, workspace=None):
     """x W^T + bias, x (rows as in mx4_quantize) quantised on the way; w: mx4_quantize of the weights [n, k]."""
     torch = _torch or _import_torch()
-    xv = _matrix(x, "x")
-    m, k = xv.B * xv.rows, xv.heads * xv.cols
-    out, v = _product_out(out, out_dtype, m, n, x.device)
+    xv, m, k = _matrix(x, "x")
+    out, v = _product_out(out, out_dtype, m, n, x)
     if workspace is None:
         workspace = torch.empty(mx4_linear_bytes(m, k), dtype=torch.uint8, device=x.device)
-    _here(x, w, bias, out, workspace)
+    stream = _here(x, w, bias, out, workspace)
     _whole(w, torch.uint8, mx4_bytes(n, k), "w")
     if bias is not None:
         _whole(bias, torch.float32, n, "bias")
     _check(lib().fps_mx4_linear(xv, w.data_ptr(), _ptr(bias), v, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                _stream()))
+                                stream))
     return out

@@ -202,7 +202,7 @@ def test_the_binding_refuses_products():
         with pytest.raises(ValueError, match="not a matrix"):
             fps.mx4_linear(x, w, 9, out=out)
     three = torch.zeros(2, 5, 70)[:, 1:]
-    assert [getattr(fps._matrix(three, "x"), n) for n in ("B", "heads", "rows", "cols", "stride_b", "stride_r")] == [2, 1, 4, 70, 350, 70]
+    assert [getattr(fps._matrix(three, "x")[0], n) for n in ("B", "heads", "rows", "cols", "stride_b", "stride_r")] == [2, 1, 4, 70, 350, 70]
 
 
 def test_the_build_links_objects_alone(tmp_path, monkeypatch):
