@@ -222,13 +222,14 @@ constexpr int kWhole = -1, kStaged = 1024;
 // which the next one's rows are on their way while one is worked on.
 constexpr int kManyHeads = 4;
 struct Units { int heads, parts, count; uint32_t rc; };      // heads of a workgroup, workgroups for all heads; groups (blocks) of a head
-template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED, bool MANY, bool PAST>
+template <int BS, int THREADS, bool IN32, bool HALVES, bool FP8, int NB, int PASS, bool STAGED, bool MANY, bool PAST, bool OWN>
 __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows x, Turning k, uint8_t* __restrict__ xq,
                                                                            float* __restrict__ scales, int role, Geom g,
                                                                            int heads, Units units) {
     constexpr int U = BS * 8 / THREADS, WAVES = THREADS * NB / 64;
     __shared__ uint32_t red[2][WAVES];                        // of one head and the next
     __shared__ __attribute__((aligned(16))) float4 staged[STAGED ? kStaged : 1];
+    __shared__ __attribute__((aligned(16))) float weights[OWN ? kManyHeads * 128 : 1];      // OWN: of the workgroup's heads, not in the staged turns
     const int kb = NB > 1 ? (int)threadIdx.x / THREADS : 0, tid = threadIdx.x - kb * THREADS, u = tid & 7;
     load_arguments<6>();
     const int bp = quotient(blockIdx.x, units.count, units.rc), b = bp / units.parts, head0 = (bp - b * units.parts) * units.heads;
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         const bool turns = org.box.n > 0 && (axis < 2 || q < k.cw);
         const float2* table = reinterpret_cast<const float2*>(k.table + b * k.table_b);
         const float* w = k.weight + head0 * k.weight_head + a;
-        const float wa = k.weight ? w[0] : 1.0f, wb = k.weight ? w[HALVES ? 64 : 1] : 1.0f;
+        const float wa = k.weight && !OWN ? w[0] : 1.0f, wb = k.weight && !OWN ? w[HALVES ? 64 : 1] : 1.0f;
         constexpr int R = THREADS * NB / 64, L = 4;          // places at a time, loads at a time
         for (int first = threadIdx.x >> 6; first < places; first += L * R) {
             float2 cs[L];
@@ -276,6 +277,8 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                                                                : make_float4(cs[l].x, cs[l].y, wa, wb);
         }
     }
+    if (OWN)
+        for (int i = threadIdx.x; i < (last_head - head0 + 1) * 128; i += THREADS * NB) weights[i] = k.weight[head0 * 128 + i];
     if (STAGED) __syncthreads();
     auto turned = [&](const Pairs& v, const Offset& d, int head) __attribute__((always_inline)) {
         if (!STAGED) return weighted_turned(v, load_weight<IN32, HALVES>(k, head, u),
@@ -316,8 +319,18 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 continue;
             }
             const Pairs v = unpack<IN32, HALVES>(now[i]);
-            y[i] = turned(v, token[i], head);
-            r[i] = inverse_rms(k, v);
+            if (OWN) {
+                r[i] = inverse_rms(k, v);                    // here: behind the rotation it takes registers for 16 more values, 720p 263 us
+                const float* w = weights + (head - head0) * 128;
+                const Pairs by = pairs_of<HALVES>([&](int s) __attribute__((always_inline)) { return w[channel_of<IN32>(u, s)]; });
+                Pairs z;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { z.a[j] = v.a[j] * by.a[j]; z.b[j] = v.b[j] * by.b[j]; }
+                y[i] = turned(z, token[i], head);
+            } else {
+                y[i] = turned(v, token[i], head);
+                r[i] = inverse_rms(k, v);
+            }
             if (FP8 && PASS != 1) {
                 float m = 0.0f;
 #pragma unroll
@@ -626,7 +639,7 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate launch");
 }
 
-template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY, bool PAST>
+template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY, bool PAST, bool OWN>
 static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                            hipStream_t st) {
     // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
@@ -640,14 +653,14 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
     const Launch blocks = of_head(g.M * g.KB, MANY);
     const int groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY, PAST><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY, PAST, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         return;
     }
     auto whole = [&](auto nb) {
         constexpr int NB = decltype(nb)::value, T = TH * NB > 1024 ? TH / 2 : TH;
         constexpr bool many = MANY && T == TH;               // twice the rows a lane: no registers for the next head's
         const Launch l = of_head(g.M * g.NS, many);
-        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many, many && PAST><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
+        norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many, many && PAST, many && OWN><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
     };
     if (g.KBS == 1)      whole(Count<1>{});
     else if (g.KBS == 2) whole(Count<2>{});
@@ -655,8 +668,8 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
     else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
         if (g.KBS == 4) return whole(Count<4>{});            // 512 tokens, 1024 threads: one pass instead of two and three launches less
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);     // x is read twice: by way of the caches
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY, false><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
-        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY, false><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
+        norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         amax_to_scale_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
 }
@@ -665,22 +678,24 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
                                int prec, void* xq, float* scales, hipStream_t st) {
     const Turning k = turning_of(g, norm, rot);
     const bool staged = (long long)g.Qt * k.ct + (long long)g.Qh * k.ch + (long long)g.Qw * (64 - k.ct - k.ch) <= kStaged;
-    // Several heads a workgroup where there are 1024 blocks of 128 slots or more (bf16, one weight for all: the staged turns hold
-    // it; fp32 rows leave no registers).  us with one head, with four: 480p of 12 heads 38.9, 32.7 (BF16 48.8, 43.8), 720p of 40 heads 247,
-    // 227 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12 heads, 540 blocks of 128, 9.6, 11.1
-    const bool many = staged && x.heads > 1 && !k.weight_head && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
     // past the caches: 720p of 40 heads 228 -> 210 us (BF16 306 -> 296); 480p of 12, which they hold, 33.4, 36.3
     const bool past = (long long)x.B * x.heads * x.rows * kHeadDim * (prec == FPS_PREC_FP8 ? 3 : 4) > kCaches;
-    auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn, auto pa) {
-        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value, decltype(pa)::value>(
+    // Several heads a workgroup where there are 1024 blocks of 128 slots or more (bf16; fp32 rows leave no registers).  us with one head,
+    // with four: 480p of 12 heads 38.9, 32.7 (BF16 48.8, 43.8), 720p of 40 heads 247, 227 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12
+    // heads, 540 blocks of 128, 9.6, 11.1.  With weights of each head, which the staged turns then do not hold, beyond the caches: 720p 239, 215
+    // (313, 298); 480p 35.0, 36.4
+    const bool own = k.weight_head != 0, many = staged && x.heads > 1 && (!own || past) && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
+    auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn, auto pa, auto ow) {
+        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value, decltype(pa)::value, decltype(ow)::value>(
             g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
     };
     with(g.BS == 128, [&](auto big) { with(halves(rot), [&](auto hv) {
         const std::true_type yes;
         const std::false_type no;
-        if (x.dt == FPS_OUT_F32) with(staged, [&](auto sg) { launch(big, yes, hv, sg, no, no); });
-        else if (many)           with(past, [&](auto pa) { launch(big, no, hv, yes, yes, pa); });
-        else                     with(staged, [&](auto sg) { launch(big, no, hv, sg, no, no); });
+        if (x.dt == FPS_OUT_F32) with(staged, [&](auto sg) { launch(big, yes, hv, sg, no, no, no); });
+        else if (many && own)    launch(big, no, hv, yes, yes, yes, yes);
+        else if (many)           with(past, [&](auto pa) { launch(big, no, hv, yes, yes, pa, no); });
+        else                     with(staged, [&](auto sg) { launch(big, no, hv, sg, no, no, no); });
     }); });
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");

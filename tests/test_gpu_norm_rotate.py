@@ -168,6 +168,10 @@ OPERANDS = [
     dict(grid=(9, 60, 70), tile=(1, 8, 16), heads=5, B=2, layout="fused", weight="per_head"),
     dict(grid=(16, 61, 67), tile=(1, 8, 16), heads=11, layout="fused", halves=True),           # beyond 256 MB in and out together
     dict(grid=(16, 61, 67), tile=(4, 16, 16), heads=11),
+    dict(grid=(16, 61, 67), tile=(1, 8, 16), heads=11, layout="fused", weight="per_head"),
+    dict(grid=(9, 60, 70), tile=(2, 8, 16), heads=6, B=2, halves=True, weight="per_head"),
+    dict(grid=(8, 60, 70), tile=(4, 16, 16), heads=7, layout="fused", weight="per_head"),
+    dict(grid=(9, 60, 70), tile=(3, 4, 4), heads=9, weight="per_head", halves=True),
 ]
 
 
