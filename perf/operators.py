@@ -289,17 +289,11 @@ def _to_four_bits(x):
     top = blocks.abs().amax(-1, keepdim=True)
     power = (torch.frexp(top).exponent - 3).clamp(-127, 127)      # floor(log2) - 2
     power = torch.where(top == 0, torch.zeros_like(power), power)
-    unit = _power_of_two(power)
-    v = blocks / unit
+    v = torch.ldexp(blocks, -power)
     size = v.abs()
     step = torch.where(size < 2, 0.5, torch.where(size < 4, 1.0, 2.0))
     v = ((v / step).round() * step).clamp(-6, 6)
-    return (v * unit).reshape(rows, -1)[:, :K]
-
-
-def _power_of_two(e):
-    """2^e in fp32 exactly, from -127 to 127."""
-    return ((e.clamp_min(-126) + 127) << 23).to(torch.int32).view(torch.float32) * torch.where(e < -126, 0.5, 1.0)
+    return torch.ldexp(v, power).reshape(rows, -1)[:, :K]
 
 
 def _weight_of_heads(weight, c):
@@ -344,8 +338,7 @@ def _exact_four_bits(x):
         n = b.shape[0]
         b = torch.cat((b, b.new_zeros(n, -K % 32)), 1).view(n, -1, 32)
         top = b.abs().max(2, keepdim=True).values
-        power = (top.clamp_min(1e-300).log2().floor() - 2).clamp(-127, 127)
-        unit = ((torch.where(top > 0, power, torch.zeros_like(power)).long() + 1023) << 52).view(torch.float64)     # 2^power
+        unit = torch.where(top > 0, 2.0 ** (top.clamp_min(1e-300).log2().floor() - 2).clamp(-127, 127), torch.ones_like(top))
         out[r:r + part] = (levels[_nearest_e2m1(b.abs() / unit)] * b.sign() * unit).view(n, -1)[:, :K]
     return out
 
