@@ -308,7 +308,7 @@ int fps_rotation_table_host(const fps_shape* shape, const fps_rotation* rot, con
  * aligned (strides are multiples of 8 elements in bf16, 4 in fp32).  norm or rot may be NULL: without that step.  Computed in
  * fp32 and rounded once, at the end.  y may be x itself (the same data, type and strides).  Of shape the grid, B and heads
  * count; its tile only has to be valid.  A row that holds an infinity or a NaN gives such values itself and leaves the other rows
- * alone; one whose squares' sum passes fp32's range (magnitudes about 2^64) counts as infinitely long and gives zeros. */
+ * alone; one whose squares' sum passes fp32's range (magnitudes about 2^64 and above) counts as infinitely long and gives zeros. */
 int fps_norm_rotate(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
                     const fps_view* y, void* stream);
 
@@ -325,7 +325,7 @@ size_t fps_norm_rotate_bwd_bytes(const fps_shape* shape, const fps_norm* norm);
 /* The gradient of fps_norm_rotate: from x and dy, the gradient of y, dx and, unless it is NULL, dweight (device, fp32,
  * shaped like norm->weight; NULL where that is; summed over all tokens, batches and, if the heads share a weight, heads, in an order that only the
  * shape determines).  x, dy and dx have one type; dx may be x or dy itself.  Quantisation by fps_norm_rotate_operand
- * is passed straight through by the same call.  workspace: device memory of fps_norm_rotate_bwd_bytes(), free again when the
+ * is passed straight through by the same call.  A row that counts as infinitely long has no gradient.  workspace: device memory of fps_norm_rotate_bwd_bytes(), free again when the
  * call has run; FPS_ERR_WORKSPACE if it is smaller. */
 int fps_norm_rotate_bwd(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
                         const fps_view* dy, const fps_view* dx, float* dweight, void* workspace, size_t workspace_bytes,

@@ -2,7 +2,7 @@
 // straight into the packed operands of the attention; the gradient of both; and the values of packed E4M3 operands.
 //
 //   y = R(t,h,w) (x r w),  r = (mean x^2 + eps)^(-1/2),  R: 64 rotations of pairs of channels
-//   g = R^T dy,  dw = sum g x r,  dx = r (g w - x r^2 mean(g w x))
+//   n = x r,  g = R^T dy,  dw = sum g n,  dx = r (g w - n mean(g w n))
 //
 // All of it is bound by HBM: some ten operations an element.  Eight lanes hold a row of 128 channels, 16 channels or 8
 // pairs each, so that a row is two (four) 16-byte loads of each lane, the sum over it three exchanges between neighbouring
@@ -170,12 +170,12 @@ __device__ __forceinline__ float inverse_rms(const Turning& k, const Pairs& x) {
     for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x.a[i], x.a[i], __builtin_fmaf(x.b[i], x.b[i], s));
     return __builtin_amdgcn_rsqf(row_sum(s) * (1.0f / 128.0f) + k.eps);
 }
-// R (x w), which r is left to be multiplied with
-__device__ __forceinline__ Pairs weighted_turned(const Pairs& x, const Pairs& w, const Turn& turn) {
+// R (n w) of a normed row n = x r: r first, so that nothing that follows passes fp32's range, and a row whose squares do, r = 0, gives zeros
+__device__ __forceinline__ Pairs weighted_turned(const Pairs& n, const Pairs& w, const Turn& turn) {
     Pairs y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float a = x.a[i] * w.a[i], b = x.b[i] * w.b[i];
+        const float a = n.a[i] * w.a[i], b = n.b[i] * w.b[i];
         y.a[i] = __builtin_fmaf(a, turn.c[i], -(b * turn.s[i]));
         y.b[i] = __builtin_fmaf(a, turn.s[i], b * turn.c[i]);
     }
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
     for (int i = 0; i < HC; ++i) {
         if (h0 + i >= heads) break;
         const Pairs w = load_weight<IN32, HALVES>(k, h0 + i, u), v = unpack<IN32, HALVES>(c[i]);
-        store_row<IN32, OUT32, HALVES, PAST>(const_cast<char*>(y.at(b, h0 + i, n)), u, times(weighted_turned(v, w, turn), inverse_rms(k, v)));
+        store_row<IN32, OUT32, HALVES, PAST>(const_cast<char*>(y.at(b, h0 + i, n)), u, weighted_turned(times(v, inverse_rms(k, v)), w, turn));
     }
 }
 
@@ -306,21 +306,18 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 if (org.slot0 + kb * BS + (tid >> 3) + THREADS / 8 * i < org.box.n) ahead[i] = load_row<IN32, PAST>(from[i], u);
             }
         }
-        Pairs y[U];                                              // without the norm's factor r of the row
-        float r[U];
-        uint32_t top = 0;                                        // magnitudes order like their bits, NaN above all
+        Pairs y[U];
+        float m = 0.0f;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             // a wave's rows of padding alone: tile (4,16,16), half of it outside the grid, 190 -> 172 us, BF16 of 480p 44.4 -> 41.3
             if (org.slot0 + kb * BS + (__builtin_amdgcn_readfirstlane(tid >> 6) << 3) + THREADS / 8 * i >= org.box.n) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
-                r[i] = 1.0f;
                 continue;
             }
-            const Pairs v = unpack<IN32, HALVES>(now[i]);
+            const Pairs x0 = unpack<IN32, HALVES>(now[i]), v = times(x0, inverse_rms(k, x0));
             if (OWN) {
-                r[i] = inverse_rms(k, v);                    // here: behind the rotation it takes registers for 16 more values, 720p 263 us
                 const float* w = weights + (head - head0) * 128;
                 const Pairs by = pairs_of<HALVES>([&](int s) __attribute__((always_inline)) { return w[channel_of<IN32>(u, s)]; });
                 Pairs z;
@@ -329,22 +326,19 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 y[i] = turned(z, token[i], head);
             } else {
                 y[i] = turned(v, token[i], head);
-                r[i] = inverse_rms(k, v);
             }
             if (FP8 && PASS != 1) {
-                float m = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) m = max_magnitude(m, y[i].a[j], y[i].b[j]);
-                const uint32_t of_row = __float_as_uint(m * r[i]) & 0x7FFFFFFFu;                        // rounds like the largest product
-                top = top > of_row ? top : of_row;
             }
         }
+        uint32_t top = __float_as_uint(m) & 0x7FFFFFFFu;         // magnitudes order like their bits, NaN above all
         char* const dst = (char*)xq + (long long)blk * (BS * 128 * (FP8 ? 1 : 2));
         if constexpr (!FP8) {                                    // 8 channels are a chunk of 16 bytes
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 const int j = (tid >> 3) + THREADS / 8 * i;
-                const Pairs z = times(y[i], r[i]);
+                const Pairs& z = y[i];
                 const bool real = org.slot0 + kb * BS + j < org.box.n;               // padding is 0, not -0
                 auto two = [&](int s) __attribute__((always_inline)) { return real ? pack_bf16(slot_of<HALVES>(z, s & 15), slot_of<HALVES>(z, (s + 1) & 15)) : 0u; };
                 auto chunk = [&](int c8) { return role == FPS_ROLE_K ? ((j >> 5) * 8 + (c8 >> 1)) * 64 + 32 * (c8 & 1) + (j & 31) : j * 16 + c8; };
@@ -374,7 +368,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int j = (tid >> 3) + THREADS / 8 * i;
-            const Pairs z = times(up == 1.0f ? y[i] : times(y[i], up), r[i] * rs);         // |x| <= amax: the product cannot reach the next code, 480
+            const Pairs z = times(up == 1.0f ? y[i] : times(y[i], up), rs);         // |x| <= amax: the product cannot reach the next code, 480
             // the 16-byte chunk of channels 16 c16 ..
             auto chunk = [&](int c16) {
                 return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
@@ -437,24 +431,25 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             const Pairs xv = unpack<F32, HALVES>(cx[i]), g0 = unpack<F32, HALVES>(cy[i]);
             Pairs& sum = dw[OWN ? i : 0];
             const float r = inverse_rms(k, xv);
+            const Pairs nv = times(xv, r);                   // at most the row's length: no product below passes fp32's range by x
             Pairs g;
             float dot = 0.0f;
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
                 const float ga = __builtin_fmaf(g0.a[m], turn.c[m], g0.b[m] * turn.s[m]);
                 const float gb = __builtin_fmaf(g0.b[m], turn.c[m], -(g0.a[m] * turn.s[m]));
-                sum.a[m] = __builtin_fmaf(ga, xv.a[m] * r, sum.a[m]);
-                sum.b[m] = __builtin_fmaf(gb, xv.b[m] * r, sum.b[m]);
+                sum.a[m] = __builtin_fmaf(ga, nv.a[m], sum.a[m]);
+                sum.b[m] = __builtin_fmaf(gb, nv.b[m], sum.b[m]);
                 g.a[m] = ga * w.a[m];
                 g.b[m] = gb * w.b[m];
-                dot = __builtin_fmaf(g.a[m], xv.a[m], __builtin_fmaf(g.b[m], xv.b[m], dot));
+                dot = __builtin_fmaf(g.a[m], nv.a[m], __builtin_fmaf(g.b[m], nv.b[m], dot));
             }
-            const float back = k.norm ? row_sum(dot) * (1.0f / 128.0f) * r * r : 0.0f;
+            const float back = k.norm ? row_sum(dot) * (1.0f / 128.0f) : 0.0f;
             Pairs d;
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
-                d.a[m] = r * __builtin_fmaf(-xv.a[m], back, g.a[m]);
-                d.b[m] = r * __builtin_fmaf(-xv.b[m], back, g.b[m]);
+                d.a[m] = r * __builtin_fmaf(-nv.a[m], back, g.a[m]);
+                d.b[m] = r * __builtin_fmaf(-nv.b[m], back, g.b[m]);
             }
             store_row<F32, F32, HALVES, PAST>(const_cast<char*>(dx.at(b, h0 + i, n)), u, d);
         }
