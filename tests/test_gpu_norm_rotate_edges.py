@@ -8,6 +8,11 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+LONG = [dict(grid=(3, 9, 20), tile=(1, 8, 16), dt=BF16), dict(grid=(3, 9, 20), tile=(4, 16, 16), dt=F32, halves=True),
+        dict(grid=(5, 18, 33), tile=(1, 8, 16), heads=9, dt=BF16, weight="per_head"),
+        dict(grid=(9, 60, 70), tile=(1, 8, 16), heads=5, layout="fused")]
+
+
 @pytest.mark.parametrize("case", LONG)
 def test_rows_whose_squares_pass_fp32_are_infinitely_long(case):
     """r is 0 then: zeros out and no gradient, however large the row, its weights and its gradient are; other rows keep their bits."""
