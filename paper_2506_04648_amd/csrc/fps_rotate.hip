@@ -168,16 +168,19 @@ __device__ __forceinline__ float inverse_rms(const Turning& k, const Pairs& x) {
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x.a[i], x.a[i], __builtin_fmaf(x.b[i], x.b[i], s));
-    return __builtin_amdgcn_rsqf(row_sum(s) * (1.0f / 128.0f) + k.eps);
+    return __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum(s), 1.0f / 128.0f, k.eps));
 }
-// R (n w) of a normed row n = x r: r first, so that nothing that follows passes fp32's range, and a row whose squares do, r = 0, gives zeros
+// R w: what a pair of a normed row n = x r is multiplied with, y = (n_a x - n_b y, n_a z + n_b w).  r comes first, so that nothing that
+// follows passes fp32's range, and a row whose squares do, r = 0, gives zeros.  Every kernel has these products and this order, so
+// that a value has the same bits wherever it is asked for.
+__device__ __forceinline__ float4 weighted(float wa, float wb, float cos, float sin) { return make_float4(wa * cos, wb * sin, wa * sin, wb * cos); }
 __device__ __forceinline__ Pairs weighted_turned(const Pairs& n, const Pairs& w, const Turn& turn) {
     Pairs y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float a = n.a[i] * w.a[i], b = n.b[i] * w.b[i];
-        y.a[i] = __builtin_fmaf(a, turn.c[i], -(b * turn.s[i]));
-        y.b[i] = __builtin_fmaf(a, turn.s[i], b * turn.c[i]);
+        const float4 f = weighted(w.a[i], w.b[i], turn.c[i], turn.s[i]);
+        y.a[i] = __builtin_fmaf(n.a[i], f.x, -(n.b[i] * f.y));
+        y.b[i] = __builtin_fmaf(n.a[i], f.z, n.b[i] * f.w);
     }
     return y;
 }
@@ -215,8 +218,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(Rows x, Rows y, Turnin
 // reads x again, encodes.
 // A token's cosines and sines would be four times as many load instructions as its channels, and all the arithmetic is as long as the
 // memory takes: where the entries of the group's planes, rows and columns, those of the columns filled up to 64 pairs, are at most
-// kStaged (STAGED) they are brought into LDS first, for FP8 multiplied by the pair's weights: (x, y) -> (x A - y B, x C + y D).  (BF16
-// operands are, bit for bit, the packed bf16 tensor, and take the products in its order.)
+// kStaged (STAGED) they are brought into LDS first, multiplied by the pair's weights.  (Operands are, bit for bit, those of the raster
+// tensor, in fp32 for FP8, in bf16 for BF16.)
 constexpr int kWhole = -1, kStaged = 1024;
 // Half of a wave's instructions find its tokens and stage the turns.  MANY: they are for kManyHeads heads, one after the other, of
 // which the next one's rows are on their way while one is worked on.
@@ -273,8 +276,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
 #pragma unroll
             for (int l = 0; l < L; ++l)
                 if (first + l * R < places)
-                    staged[to + (first + l * R) * c + q] = FP8 ? make_float4(wa * cs[l].x, wb * cs[l].y, wa * cs[l].y, wb * cs[l].x)
-                                                               : make_float4(cs[l].x, cs[l].y, wa, wb);
+                    staged[to + (first + l * R) * c + q] = weighted(wa, wb, cs[l].x, cs[l].y);
         }
     }
     if (OWN)
@@ -283,15 +285,17 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
     auto turned = [&](const Pairs& v, const Offset& d, int head) __attribute__((always_inline)) {
         if (!STAGED) return weighted_turned(v, load_weight<IN32, HALVES>(k, head, u),
                                             load_turn<IN32, HALVES>(k, b, min_of(n0 + (d.t * g.H + d.h) * g.W + d.w, g.T * g.H * g.W - 1), u));
-        Pairs y;
         const int at_t = d.t * k.ct, at_h = of_t + d.h * k.ch - k.ct, at_w = of_t + of_h + d.w * rest - k.ct - k.ch;
+        Pairs by;
+        if (OWN) by = pairs_of<HALVES>([&](int s) __attribute__((always_inline)) { return weights[(head - head0) * 128 + channel_of<IN32>(u, s)]; });
+        Pairs y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int p = pair_of<IN32, HALVES>(u, i);
-            const float4 f = staged[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
-            const float a = FP8 ? v.a[i] : v.a[i] * f.z, b = FP8 ? v.b[i] : v.b[i] * f.w;
-            y.a[i] = __builtin_fmaf(a, f.x, -(b * f.y));
-            y.b[i] = __builtin_fmaf(a, FP8 ? f.z : f.y, b * (FP8 ? f.w : f.x));
+            float4 f = staged[(p < k.ct ? at_t : p < k.ct + k.ch ? at_h : at_w) + p];
+            if (OWN) f = weighted(by.a[i], by.b[i], f.x, f.y);
+            y.a[i] = __builtin_fmaf(v.a[i], f.x, -(v.b[i] * f.y));
+            y.b[i] = __builtin_fmaf(v.a[i], f.z, v.b[i] * f.w);
         }
         return y;
     };
@@ -317,16 +321,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 continue;
             }
             const Pairs x0 = unpack<IN32, HALVES>(now[i]), v = times(x0, inverse_rms(k, x0));
-            if (OWN) {
-                const float* w = weights + (head - head0) * 128;
-                const Pairs by = pairs_of<HALVES>([&](int s) __attribute__((always_inline)) { return w[channel_of<IN32>(u, s)]; });
-                Pairs z;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { z.a[j] = v.a[j] * by.a[j]; z.b[j] = v.b[j] * by.b[j]; }
-                y[i] = turned(z, token[i], head);
-            } else {
-                y[i] = turned(v, token[i], head);
-            }
+            y[i] = turned(v, token[i], head);
             if (FP8 && PASS != 1) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) m = max_magnitude(m, y[i].a[j], y[i].b[j]);

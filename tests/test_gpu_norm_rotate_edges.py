@@ -2,7 +2,8 @@
 import pytest
 
 from paper_2506_04648_amd import fps
-from tests.test_gpu_norm_rotate import BF16, DEV, F32, Case, say
+from tests import operators_plain as op
+from tests.test_gpu_norm_rotate import BF16, DEV, F32, OPERANDS, Case, say
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,31 @@ def test_rows_whose_squares_pass_fp32_are_infinitely_long(case):
     quiet = torch.where(rows[..., None], torch.zeros_like(dy), dy)
     other, want = fps.norm_rotate_bwd(c.shape, short, quiet, c.norm, c.rotation)
     assert torch.equal(dx[~rows], other[~rows]) and torch.equal(dw, want)
+
+
+@pytest.mark.parametrize("case", OPERANDS)
+def test_fp8_scales_are_those_of_the_raster_values(case):
+    """amax / 448 of what norm_rotate gives in fp32, bit for bit, whichever kernel a call takes.  (A quotient of two 24-bit numbers
+    rounded to 53 bits and then to 24 is the one rounded once.)"""
+    say("scales", case)
+    c = Case(**case)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out_dtype=F32).reshape(c.x.shape)
+    group, n = op.group_of_tokens(c.grid, case["tile"], case.get("qtile"))
+    top = torch.zeros(c.B, c.heads, n, device=DEV).scatter_reduce_(2, group.to(DEV).expand(c.B, c.heads, -1), y.abs().amax(-1), "amax")
+    want = torch.where(top == 0, 1.0, (top.double() / 448).float())
+    for role in (fps.ROLE_Q, fps.ROLE_K):
+        assert torch.equal(fps.norm_rotate_operand(c.shape, c.x, role, fps.PREC_FP8, c.norm, c.rotation)[1], want)
+
+
+@pytest.mark.parametrize("case", [c for c in OPERANDS if c.get("heads", 2) > 4])
+def test_operands_of_a_head_do_not_depend_on_the_others(case):
+    """Codes and scales of all heads in one call are those of each head in a call of its own."""
+    say("heads", case)
+    c = Case(**case)
+    packed, scales = fps.norm_rotate_operand(c.shape, c.x, fps.ROLE_K, fps.PREC_FP8, c.norm, c.rotation)
+    packed = packed.view(c.B, c.heads, -1)
+    alone = fps.make_shape(1, c.grid, case["tile"], B=c.B, qtile=case.get("qtile"))
+    for h in range(c.heads):
+        norm = fps.make_norm(c.weight[h:h + 1].clone(), 1e-6) if case.get("weight") == "per_head" else c.norm
+        p, s = fps.norm_rotate_operand(alone, c.x[:, h:h + 1], fps.ROLE_K, fps.PREC_FP8, norm, c.rotation)
+        assert torch.equal(s[:, 0], scales[:, h]) and torch.equal(p.view(c.B, -1), packed[:, h]), h
