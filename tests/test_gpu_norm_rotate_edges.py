@@ -73,3 +73,19 @@ def test_operands_of_a_head_do_not_depend_on_the_others(case):
         norm = fps.make_norm(c.weight[h:h + 1].clone(), 1e-6) if case.get("weight") == "per_head" else c.norm
         p, s = fps.norm_rotate_operand(alone, c.x[:, h:h + 1], fps.ROLE_K, fps.PREC_FP8, norm, c.rotation)
         assert torch.equal(s[:, 0], scales[:, h]) and torch.equal(p.view(c.B, -1), packed[:, h]), h
+
+
+@pytest.mark.parametrize("case", OPERANDS)
+@pytest.mark.parametrize("role", [fps.ROLE_Q, fps.ROLE_K])
+def test_fp8_codes_are_those_of_the_quotient(case, role):
+    """Every code is the one nearest to the fp32 quotient of norm_rotate's value and the scale, halfway cases to even."""
+    say("codes", case, role)
+    c = Case(**case)
+    y = fps.norm_rotate(c.shape, c.x, c.norm, c.rotation, out_dtype=F32).reshape(c.x.shape)
+    group, _ = op.group_of_tokens(c.grid, case["tile"], case.get("qtile"))
+    packed, scales = fps.norm_rotate_operand(c.shape, c.x, role, fps.PREC_FP8, c.norm, c.rotation)
+    codes = fps.tile_unorder(c.shape, fps.debug_unpack_q8(c.shape, packed, role).view(torch.float8_e4m3fn).float()).reshape(y.shape)
+    for h in range(c.heads):
+        s = scales[:, h].gather(1, group.to(DEV).expand(c.B, -1))[..., None]
+        want = (y[:, h].double() / s.double()).float().to(torch.float8_e4m3fn).float()
+        assert bool((codes[:, h] == want).all()), (h, int((codes[:, h] != want).sum()))
