@@ -23,7 +23,8 @@ def build_lib(verbose: bool = False) -> str:
              # packed fp32 instructions stay off (they are generated from ordinary float code otherwise)
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
              # no NaN ever enters the attention (inputs are finite, masked scores are -inf, never inf-inf): lets fmax/fmin
-             # compile without the canonicalising v_max(x,x) in front of every operand; the other kernels and the host compare bits
+             # compile without the canonicalising v_max(x,x) in front of every operand; what
+             # may meet one, around the attention and on the host, compares bits
              "-fno-honor-nans"] + os.environ.get("FPS_EXTRA_HIPCC_FLAGS", "").split()
     # MFMA results stay in architectural VGPRs: the softmax VALU code reads them directly instead of through
     # v_accvgpr moves

@@ -191,6 +191,8 @@ __device__ __forceinline__ Pairs times(const Pairs& y, float r) {
     return z;
 }
 
+// the scale of a group whose largest magnitude has the bits `top`, which are compared: a NaN's is NaN
+__device__ __forceinline__ float scale_of(uint32_t top) { return top == 0 ? 1.0f : __uint_as_float(top) / 448.0f; }
 __device__ __forceinline__ float quotient_by(float x, float s, float rs) {
     const float q = x * rs;
     return __builtin_fmaf(__builtin_fmaf(-q, s, x), rs, q);
@@ -361,7 +363,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
                 continue;
             }
         }
-        const float amax = __uint_as_float(top), s = top == 0 ? 1.0f : amax / 448.0f;
+        const float s = scale_of(top);
         if (PASS == kWhole && threadIdx.x == 0) scales[group] = s;
         // a scale near the end of the range: its reciprocal would pass it
         const float up = s < 0x1p-60f ? 0x1p64f : 1.0f, s1 = s * up, rs = 1.0f / s1;
@@ -397,6 +399,12 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
             }
         }
     }
+}
+
+// the maxima that PASS 0 found to scales
+__global__ void scales_kernel(float* p, int n) {
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) p[i] = scale_of(__float_as_uint(p[i]));
 }
 
 // ---- the gradient -------------------------------------------------------------------------------
@@ -672,7 +680,7 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);     // x is read twice: by way of the caches
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
-        amax_to_scale_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
+        scales_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
 }
 

@@ -89,3 +89,28 @@ def test_fp8_codes_are_those_of_the_quotient(case, role):
         s = scales[:, h].gather(1, group.to(DEV).expand(c.B, -1))[..., None]
         want = (y[:, h].double() / s.double()).float().to(torch.float8_e4m3fn).float()
         assert bool((codes[:, h] == want).all()), (h, int((codes[:, h] != want).sum()))
+
+
+@pytest.mark.parametrize("tile", [(1, 8, 16), (3, 4, 4), (2, 8, 16), (8, 8, 8), (4, 16, 16)])
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("norm", [True, False])
+def test_groups_with_infinities_and_nans_have_such_a_scale(tile, dt, norm):
+    """And the other groups are as they were."""
+    c = Case(grid=(9, 18, 33), tile=tile, dt=dt, heads=3, norm=norm)
+    group, n = op.group_of_tokens(c.grid, tile)
+    packed, scales = fps.norm_rotate_operand(c.shape, c.x, fps.ROLE_K, fps.PREC_FP8, c.norm, c.rotation)
+    bad = torch.zeros(1, 3, n, dtype=torch.bool)
+    x = c.x.clone()
+    for h, token, channel, value in ((0, 3, 5, float("nan")), (1, 700, 127, float("inf")), (2, c.N - 1, 0, float("-inf")), (2, 1500, 64, float("nan"))):
+        x[0, h, token, channel] = value
+        bad[0, h, group[token]] = True
+    p, s = fps.norm_rotate_operand(c.shape, x, fps.ROLE_K, fps.PREC_FP8, c.norm, c.rotation)
+    bad = bad.to(DEV)
+    assert not bool(s[bad].isfinite().any()) and torch.equal(s[~bad], scales[~bad])
+    if norm:
+        assert bool(s[bad].isnan().all())
+    of_token = bad.gather(2, group.to(DEV).expand(1, 3, -1))
+    a, b = (fps.tile_unorder(c.shape, fps.debug_unpack_q8(c.shape, v, fps.ROLE_K).view(torch.float8_e4m3fn).float()).reshape(x.shape) for v in (p, packed))
+    assert torch.equal(a[~of_token], b[~of_token])
+    values = fps.dequantize(c.shape, p, s, fps.ROLE_K, out_dtype=F32).reshape(x.shape)
+    assert bool((~values.isfinite()).any(-1)[0, 0, 3])
