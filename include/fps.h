@@ -314,7 +314,8 @@ int fps_norm_rotate(const fps_shape* shape, const fps_view* x, const fps_norm* n
 
 /* Norm, rotation and operand packing of Q or K (role; V has neither) in one pass: the operands that fps_attn_fwd takes, from x
  * as in fps_norm_rotate.  FPS_PREC_FP8: as fps_quantize_raster, from the very values that fps_norm_rotate gives in fp32, whatever
- * else is in the call: scale = amax/448 of a scale group (1.0 for zeros), code = round-to-nearest-even of x/scale computed in fp32.  scales_out [B,heads,M*NS].
+ * else is in the call: scale = amax/448 of a scale group (1.0 where that is 0 in fp32), code = round-to-nearest-even of x/scale computed in
+ * fp32, saturating.  scales_out [B,heads,M*NS].
  * FPS_PREC_BF16: as fps_pack_raster_bf16; scales_out is ignored and may be NULL.  A group that holds an infinity or a NaN has such a scale. */
 int fps_norm_rotate_operand(const fps_shape* shape, const fps_view* x, const fps_norm* norm, const fps_rotation* rot,
                             fps_role role, fps_precision prec, void* xq_out, float* scales_out, void* stream);

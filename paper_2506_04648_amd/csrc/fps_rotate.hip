@@ -191,11 +191,33 @@ __device__ __forceinline__ Pairs times(const Pairs& y, float r) {
     return z;
 }
 
-// the scale of a group whose largest magnitude has the bits `top`, which are compared: a NaN's is NaN
-__device__ __forceinline__ float scale_of(uint32_t top) { return top == 0 ? 1.0f : __uint_as_float(top) / 448.0f; }
-__device__ __forceinline__ float quotient_by(float x, float s, float rs) {
-    const float q = x * rs;
-    return __builtin_fmaf(__builtin_fmaf(-q, s, x), rs, q);
+// the scale of a group whose largest magnitude has the bits `top`, NaN of a NaN; 1 where amax / 448 is nothing in fp32
+__device__ __forceinline__ float scale_of(uint32_t top) {
+    const float s = __uint_as_float(top) / 448.0f;
+    return __float_as_uint(s) == 0 ? 1.0f : s;
+}
+__device__ __forceinline__ Pairs clamped(const Pairs& q) {
+    Pairs z;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        z.a[i] = __builtin_amdgcn_fmed3f(q.a[i], -448.0f, 448.0f);
+        z.b[i] = __builtin_amdgcn_fmed3f(q.b[i], -448.0f, 448.0f);
+    }
+    return z;
+}
+// x / s rounded once: rs is the rounded reciprocal, q a quotient to two half steps, and one step with its exact residual rounds it as a
+// division does (P. Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).  Three instructions an
+// element instead of one, 480p 34.0 -> 35.7 us, 720p 215 -> 219, for the code of the quotient itself: y (r / s) had another one at some
+// 1e-6 of the elements.
+__device__ __forceinline__ Pairs quotients(const Pairs& x, float s, float rs) {
+    auto divided = [&](float v) __attribute__((always_inline)) {
+        const float q = v * rs;
+        return __builtin_fmaf(__builtin_fmaf(-q, s, v), rs, q);
+    };
+    Pairs z;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { z.a[i] = divided(x.a[i]); z.b[i] = divided(x.b[i]); }
+    return z;
 }
 
 // ---- into the caller's layout -------------------------------------------------------------------
@@ -365,38 +387,41 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         }
         const float s = scale_of(top);
         if (PASS == kWhole && threadIdx.x == 0) scales[group] = s;
-        // a scale near the end of the range: its reciprocal would pass it
-        const float up = s < 0x1p-60f ? 0x1p64f : 1.0f, s1 = s * up, rs = 1.0f / s1;
+        float by = s, rs = 1.0f / s;
+        // A scale near the end of the range: its reciprocal would pass it, and one that has lost bits there leaves quotients beyond 448.  Such a
+        // group's codes are written again: what stands before the others' conversions, or parts them from the quotients, costs 720p 3 to 15 us.
+        const bool tiny = (uint32_t)__builtin_amdgcn_readfirstlane((int)top) < __builtin_bit_cast(uint32_t, 0x1p-52f);
+        for (int again = 0;; again = 1) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int j = (tid >> 3) + THREADS / 8 * i;
-            // The quotient rounded once: rs is the rounded reciprocal, q a quotient to two half steps, and one step with its exact residual
-            // rounds it as a division does (P. Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).
-            // Three instructions an element instead of one, 480p 34.0 -> 35.7 us, 720p 215 -> 219, for the code of the quotient itself: y (r / s)
-            // had another one at some 1e-6 of the elements.
-            const Pairs v = up == 1.0f ? y[i] : times(y[i], up);
-            Pairs z;
+            for (int i = 0; i < U; ++i) {
+                const int j = (tid >> 3) + THREADS / 8 * i;
+                const Pairs z = quotients(y[i], by, rs);
+                // the 16-byte chunk of channels 16 c16 ..
+                auto chunk = [&](int c16) {
+                    return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
+                };
+                uint32_t o[4];
 #pragma unroll
-            for (int n = 0; n < 8; ++n) { z.a[n] = quotient_by(v.a[n], s1, rs); z.b[n] = quotient_by(v.b[n], s1, rs); }
-            // the 16-byte chunk of channels 16 c16 ..
-            auto chunk = [&](int c16) {
-                return role == FPS_ROLE_K ? (((j >> 5) * 2 + (c16 >> 2)) * 2 + (c16 & 1)) * 64 + 32 * ((c16 >> 1) & 1) + (j & 31) : j * 8 + c16;
-            };
-            uint32_t o[4];
+                for (int m = 0; m < 4; ++m) {
+                    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
+                    o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
+                    o[m] = org.slot0 + kb * BS + j < org.box.n ? o[m] : 0u;              // padding is 0, not -0
+                }
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int w = __builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m), slot_of<HALVES>(z, 4 * m + 1), 0, false);
-                o[m] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(slot_of<HALVES>(z, 4 * m + 2), slot_of<HALVES>(z, 4 * m + 3), w, true);
-                o[m] = org.slot0 + kb * BS + j < org.box.n ? o[m] : 0u;              // padding is 0, not -0
+                for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
+                    const int c = channel_of<IN32>(u, 4 * m);
+                    char* at = dst + 16 * chunk(c >> 4) + (c & 15);
+                    if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
+                    else if (PAST) __builtin_nontemporal_store(u32x2{o[m], o[(m + 1) & 3]}, reinterpret_cast<u32x2*>(at));
+                    else           *reinterpret_cast<u32x2*>(at) = u32x2{o[m], o[(m + 1) & 3]};
+                }
             }
+            if (!tiny || again) break;
+            by = s * 0x1p64f;
+            rs = 1.0f / by;
 #pragma unroll
-            for (int m = 0; m < 4; m += IN32 ? 1 : 2) {
-                const int c = channel_of<IN32>(u, 4 * m);
-                char* at = dst + 16 * chunk(c >> 4) + (c & 15);
-                if (IN32) *reinterpret_cast<uint32_t*>(at) = o[m];
-                else if (PAST) __builtin_nontemporal_store(u32x2{o[m], o[(m + 1) & 3]}, reinterpret_cast<u32x2*>(at));
-                else           *reinterpret_cast<u32x2*>(at) = u32x2{o[m], o[(m + 1) & 3]};
-            }
+            for (int i = 0; i < U; ++i) y[i] = clamped(quotients(times(y[i], 0x1p64f), by, rs));
+            by = rs = 1.0f;                                  // divided already
         }
     }
 }

@@ -91,6 +91,30 @@ def test_fp8_codes_are_those_of_the_quotient(case, role):
         assert bool((codes[:, h] == want).all()), (h, int((codes[:, h] != want).sum()))
 
 
+@pytest.mark.parametrize("size", [3e-41, 1.4e-42, 1e-42, 3.2e-43, 2e-43, 1.5e-45])
+@pytest.mark.parametrize("tile", [(1, 8, 16), (3, 4, 4), (8, 8, 8), (4, 16, 16)])
+def test_scales_of_few_bits(size, tile):
+    """Groups about the smallest fp32 numbers, zeros among them: the scale is amax / 448 rounded to what fp32 has there, 1 where that is
+    nothing, and a quotient beyond 448, which is the scale's rounding, saturates."""
+    c = Case(grid=(5, 18, 33), tile=tile, norm=False, rotate=False, dt=F32)
+    c.x.copy_((c.x.double().clamp(-1, 1) * size).float())
+    c.x[..., ::7] = 0.0
+    c.x[0, 0, 40:60] = 0.0
+    tiniest = 2.0 ** -149
+    group, n = op.group_of_tokens(c.grid, tile)
+    index = group.to(DEV).expand(1, c.heads, -1)
+    top = torch.zeros(1, c.heads, n, dtype=torch.float64, device=DEV).scatter_reduce_(2, index, c.x.double().abs().amax(-1), "amax")
+    want = (top / tiniest / 448).round() * tiniest
+    want = torch.where(want == 0, torch.ones_like(want), want)
+    s = want.gather(2, index)[..., None]
+    codes64 = (c.x.double() / s).clamp(-448, 448).float().to(torch.float8_e4m3fn).float()
+    for role in (fps.ROLE_Q, fps.ROLE_K):
+        packed, scales = fps.norm_rotate_operand(c.shape, c.x, role)
+        assert torch.equal(scales.double(), want)
+        codes = fps.tile_unorder(c.shape, fps.debug_unpack_q8(c.shape, packed, role).view(torch.float8_e4m3fn).float()).reshape(c.x.shape)
+        assert bool((codes == codes64).all())
+
+
 @pytest.mark.parametrize("tile", [(1, 8, 16), (3, 4, 4), (2, 8, 16), (8, 8, 8), (4, 16, 16)])
 @pytest.mark.parametrize("dt", [BF16, F32])
 @pytest.mark.parametrize("norm", [True, False])
