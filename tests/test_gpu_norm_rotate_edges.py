@@ -138,3 +138,33 @@ def test_groups_with_infinities_and_nans_have_such_a_scale(tile, dt, norm):
     assert torch.equal(a[~of_token], b[~of_token])
     values = fps.dequantize(c.shape, p, s, fps.ROLE_K, out_dtype=F32).reshape(x.shape)
     assert bool((~values.isfinite()).any(-1)[0, 0, 3])
+
+
+# ---- sums of the weights' gradient --------------------------------------------------------------
+SUMS = [dict(grid=(9, 40, 64), heads=9, B=2), dict(grid=(9, 40, 64), heads=9, B=2, weight="per_head", layout="fused"),
+        dict(grid=(9, 40, 64), heads=9, B=2, dt=F32, halves=True), dict(grid=(9, 40, 64), heads=5, B=2, dt=F32, weight="per_head"),
+        dict(grid=(16, 61, 67), heads=9, halves=True, layout="fused"), dict(grid=(16, 61, 67), heads=9, weight="per_head"),
+        dict(grid=(1, 1, 33), heads=5, halves=True, weight="per_head"), dict(grid=(21, 30, 52), heads=13)]
+
+
+@pytest.mark.parametrize("case", SUMS)
+def test_exact_sums_of_the_weights_gradient(case):
+    """Rows of one magnitude, a power of two, small whole numbers as dy, quarter turns: x r is +-1, and every term and sum is a whole
+    number below 2^24, so that the result is exact in any order of additions.  Up to nine parts of the rows a workgroup, the last one
+    cut, and beyond the caches."""
+    say("sums", case)
+    split = (22, 21, 21)
+    c = Case(rotate=False, eps=2.0 ** -40, **case)
+    size = torch.exp2(torch.randint(-2, 4, c.x.shape[:3], generator=c.gen, device=DEV))[..., None]
+    sign = 1.0 - 2.0 * torch.randint(2, c.x.shape, generator=c.gen, device=DEV)
+    c.x.copy_(size * sign)
+    dy = torch.randint(-3, 4, c.x.shape, generator=c.gen, device=DEV).to(c.dt)
+    turn = torch.tensor([[1.0, 0.0], [0.0, 1.0], [-1.0, 0.0], [0.0, -1.0]], device=DEV)
+    table = turn[torch.randint(4, (sum(n * k for n, k in zip(c.grid, split)),), generator=c.gen, device=DEV)].contiguous()
+    rotation = fps.make_rotation(table, split, c.halves)
+    cos, sin = op.turn_of_tokens(table, c.grid, split)
+    axes = (0, 2) if c.weight.dim() == 2 else (0, 1, 2)
+    want = (op.turned(dy.double(), cos, -sin, c.halves) * sign).sum(axes)
+    assert float(want.abs().max()) < 2 ** 24 and 3 * c.B * c.N * c.heads < 2 ** 24
+    dx, dw = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, rotation)
+    assert torch.equal(dw.double(), want)
