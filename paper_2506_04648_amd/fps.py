@@ -396,6 +396,13 @@ def _whole(t, dtype, numel, name):
         raise ValueError(f"{name} must be contiguous {dtype} of {numel} elements, not {t.dtype} {tuple(t.shape)}")
 
 
+def _workspace(t):
+    """A workspace's bytes, all of which are its own."""
+    if not t.is_contiguous():
+        raise ValueError(f"a workspace must be contiguous, not {tuple(t.shape)} of strides {t.stride()}")
+    return t.numel() * t.element_size()
+
+
 def _dtype_code(t):
     if not _codes:
         torch = _torch or _import_torch()
@@ -526,16 +533,17 @@ def norm_rotate_bwd(shape: Shape, x, dy, norm: Norm = None, rotation: Rotation =
         dx = torch.empty_like(x)
     if weight is None or not need_dweight:
         dweight = workspace = None
+        size = 0
     else:
         if dweight is None:
             dweight = torch.empty_like(weight)
         _whole(dweight, torch.float32, weight.numel(), "dweight")
         if workspace is None:
             workspace = torch.empty(norm_rotate_bwd_bytes(shape, norm), dtype=torch.uint8, device=x.device)
+        size = _workspace(workspace)
     stream = _here(x, dy, dx, dweight, workspace, weight, table)
     _check(lib().fps_norm_rotate_bwd(shape, _view(x, "x"), norm, rotation, _view(dy, "dy"), _view(dx, "dx"), _ptr(dweight),
-                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                     stream))
+                                     _ptr(workspace), size, stream))
     return dx, dweight
 
 
@@ -644,10 +652,10 @@ def mx4_linear(x, w, n, bias=None, out=None, out_dtype=None, workspace=None):
     out, v = _product_out(out, out_dtype, m, n, x)
     if workspace is None:
         workspace = torch.empty(mx4_linear_bytes(m, k), dtype=torch.uint8, device=x.device)
+    size = _workspace(workspace)
     stream = _here(x, w, bias, out, workspace)
     _whole(w, torch.uint8, mx4_bytes(n, k), "w")
     if bias is not None:
         _whole(bias, torch.float32, n, "bias")
-    _check(lib().fps_mx4_linear(xv, w.data_ptr(), _ptr(bias), v, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                stream))
+    _check(lib().fps_mx4_linear(xv, w.data_ptr(), _ptr(bias), v, workspace.data_ptr(), size, stream))
     return out
