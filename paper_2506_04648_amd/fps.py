@@ -435,13 +435,14 @@ def _view(t, name) -> View:
 
 
 def make_norm(weight=None, eps=1e-6) -> Norm:
-    """Norm of each token of each head; weight: fp32 [128], or [heads, 128] for one of each head, or None."""
+    """Norm of each token of each head; weight: fp32 [128], or [heads, 128] for one of each head, or None.  The tensor is kept, and
+    each call reads it where it lies then; its type and size stay."""
     if weight is not None:
         torch = _torch or _import_torch()
         if weight.dtype != torch.float32 or weight.dim() not in (1, 2) or weight.shape[-1] != 128 or not weight.is_contiguous():
             raise ValueError(f"a norm's weight is contiguous fp32 [128] or [heads, 128], not {weight.dtype} {tuple(weight.shape)}")
     norm = Norm(_ptr(weight), weight is not None and weight.dim() == 2, eps)
-    norm.tensor = weight                                   # lives as long as the pointer to it
+    norm.tensor, norm.size = weight, None if weight is None else weight.shape
     return norm
 
 
@@ -461,26 +462,37 @@ def rotation_table(shape: Shape, split, base=10000.0, start=(0, 0, 0)):
 
 def make_rotation(table, split, halves=False) -> Rotation:
     """table: fp32 [entries, 2] (cos, sin) on the device, of T*split[0] + H*split[1] + W*split[2] entries as rotation_table
-    has them, or [B, entries, 2] for one of each batch element; halves: channel i turns with i + 64 instead of 2i with 2i + 1."""
+    has them, or [B, entries, 2] for one of each batch element, kept as a norm's weight is; halves: channel i turns with i + 64
+    instead of 2i with 2i + 1."""
     torch = _torch or _import_torch()
     if table.dtype != torch.float32 or table.dim() not in (2, 3) or table.shape[-1] != 2 or not table.is_contiguous():
         raise ValueError(f"a rotation's table is contiguous fp32 [entries, 2] or [B, entries, 2], not {table.dtype} {tuple(table.shape)}")
     rot = Rotation(table.data_ptr(), 2 * table.shape[1] if table.dim() == 3 else 0, *split, PAIRS_HALVES if halves else PAIRS_ADJACENT)
-    rot.tensor = table
+    rot.tensor, rot.size = table, table.shape
     return rot
+
+
+def _address(t, size, name):
+    """Where a tensor that is kept from call to call lies now: a parameter may have been given other memory since the last one."""
+    at = t.data_ptr()
+    if t.dtype is not _torch.float32 or t.shape != size or not t.is_contiguous() or (at == 0 and t.numel() != 0):
+        raise ValueError(f"{name} has become {t.dtype} {tuple(t.shape)}" + (" without memory" if at == 0 else ""))
+    return at
 
 
 def _check_turning(shape: Shape, norm, rotation):
     weight = table = None
-    if norm is not None:
-        weight = norm.tensor
-        if weight is not None and norm.per_head and weight.shape[0] != shape.heads:
-            raise ValueError(f"a norm's weight of {weight.shape[0]} heads, not {shape.heads}")
+    if norm is not None and norm.tensor is not None:
+        weight, size = norm.tensor, norm.size
+        norm.weight = _address(weight, size, "a norm's weight")
+        if norm.per_head and size[0] != shape.heads:
+            raise ValueError(f"a norm's weight of {size[0]} heads, not {shape.heads}")
     if rotation is not None:
-        table = rotation.tensor
+        table, size = rotation.tensor, rotation.size
+        rotation.table = _address(table, size, "a rotation's table")
         n = shape.T * rotation.pairs_t + shape.H * rotation.pairs_h + shape.W * rotation.pairs_w
-        if table.shape[-2] != n or (table.dim() == 3 and table.shape[0] != shape.B):
-            raise ValueError(f"a rotation's table {tuple(table.shape)}, not of {n} entries (of {shape.B} batch elements)")
+        if size[-2] != n or (len(size) == 3 and size[0] != shape.B):
+            raise ValueError(f"a rotation's table {tuple(size)}, not of {n} entries (of {shape.B} batch elements)")
     return weight, table
 
 

@@ -168,3 +168,20 @@ def test_exact_sums_of_the_weights_gradient(case):
     assert float(want.abs().max()) < 2 ** 24 and 3 * c.B * c.N * c.heads < 2 ** 24
     dx, dw = fps.norm_rotate_bwd(c.shape, c.x, dy, c.norm, rotation)
     assert torch.equal(dw.double(), want)
+
+
+# ---- tensors that are kept from call to call ----------------------------------------------------
+def test_weights_and_tables_that_were_given_other_memory():
+    say("other memory")
+    c = Case(grid=(3, 9, 20), tile=(1, 8, 16), heads=3, weight="per_head")
+    weight, table = torch.nn.Parameter(c.weight.clone(), requires_grad=False), c.rotation.tensor.clone()
+    norm, rotation = fps.make_norm(weight, 1e-6), fps.make_rotation(table, (22, 21, 21))
+    dy = torch.randn(c.x.shape, generator=c.gen, device=DEV).to(BF16)
+    for _ in range(3):
+        old = weight.data, table.data
+        weight.data, table.data = torch.randn(3, 128, generator=c.gen, device=DEV), table.data.roll(5, 0).contiguous()
+        old[0].fill_(7.0), old[1].fill_(7.0)
+        want = fps.make_norm(weight.data.clone(), 1e-6), fps.make_rotation(table.data.clone(), (22, 21, 21))
+        for call in (lambda n, r: (fps.norm_rotate(c.shape, c.x, n, r),), lambda n, r: fps.norm_rotate_operand(c.shape, c.x, fps.ROLE_Q, fps.PREC_FP8, n, r),
+                     lambda n, r: fps.norm_rotate_bwd(c.shape, c.x, dy, n, r)):
+            assert all(torch.equal(a, b) for a, b in zip(call(norm, rotation), call(*want)))

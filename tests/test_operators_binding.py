@@ -24,3 +24,44 @@ def test_a_workspace_owns_its_bytes(workspace):
     x = torch.zeros(1, 2, 30, 128, dtype=BF16)
     with pytest.raises(ValueError, match="workspace"):
         fps.norm_rotate_bwd(s, x, x, norm, workspace=workspace(fps.norm_rotate_bwd_bytes(s, norm)))
+
+
+# ---- tensors that are kept from call to call ----------------------------------------------------
+def calls(s, norm, rotation):
+    x = torch.zeros(1, 2, 30, 128, dtype=BF16)
+    return (lambda: fps.norm_rotate(s, x, norm, rotation), lambda: fps.norm_rotate_operand(s, x, fps.ROLE_Q, fps.PREC_FP8, norm, rotation),
+            lambda: fps.norm_rotate_bwd(s, x, x, norm, rotation))
+
+
+@pytest.mark.parametrize("heads", [0, 2])
+def test_weights_and_tables_are_read_where_they_lie(heads):
+    """A parameter's memory is another one after an assignment to .data, a cast there and back, or a load that assigns."""
+    s, size = shape(), (heads, 128) if heads else (128,)
+    weight, table = torch.nn.Parameter(torch.ones(size), requires_grad=False), torch.ones(10, 2)
+    norm, rotation = fps.make_norm(weight), fps.make_rotation(table, (1, 1, 1))
+    for i in range(3):
+        old = weight.data, table.data                        # keeps the old memory, so that the new one is another
+        weight.data, table.data = torch.zeros(size), torch.zeros(10, 2)
+        norm.weight = rotation.table = 0x10000
+        with pytest.raises(ValueError, match="current device"):
+            calls(s, norm, rotation)[i]()
+        assert norm.weight == weight.data_ptr() != old[0].data_ptr() and rotation.table == table.data_ptr() != old[1].data_ptr()
+
+
+@pytest.mark.parametrize("change", [lambda t: t.to(BF16), lambda t: t.double(), lambda t: torch.ones(t.shape[:-1] + (2 * t.shape[-1],))[..., ::2],
+                                    lambda t: torch.ones(t.shape[:-1] + (64,)), lambda t: torch.ones((3,) + t.shape)])
+def test_weights_and_tables_that_became_something_else(change):
+    s = shape()
+    for of_norm in (True, False):
+        weight, table = torch.ones(128), torch.ones(10, 2)
+        norm, rotation = fps.make_norm(weight), fps.make_rotation(table, (1, 1, 1))
+        t = weight if of_norm else table
+        t.data = change(t.data)
+        for call in calls(s, norm, rotation):
+            with pytest.raises(ValueError, match="a norm's weight has become" if of_norm else "a rotation's table has become"):
+                call()
+    weight = torch.ones(128)
+    norm = fps.make_norm(weight)
+    weight.untyped_storage().resize_(0)                      # as sharded parameters have it between their uses
+    with pytest.raises(ValueError, match="without memory"):
+        calls(s, norm, None)[0]()
