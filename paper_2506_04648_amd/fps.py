@@ -377,7 +377,13 @@ def attn_fwd(shape: Shape, window, prec, q, k, v, sq=None, sk=None, sv=None, vsc
 
 # ---- before and after the attention -------------------------------------------------------------
 def _here(*tensors):
-    """Every tensor (None: left out) is on the current device; returns its stream, which the call goes to."""
+    """Every tensor (None: left out) is on the current device and autograd waits for a gradient of none; returns its stream, which the call
+    goes to."""
+    if (_torch or _import_torch()).is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("a tensor requires a gradient, which this call does not record: make it under torch.no_grad(), or in an "
+                                 "autograd.Function whose backward calls the gradient's entry point")
     current = None
     for t in tensors:
         if t is None:
@@ -385,7 +391,7 @@ def _here(*tensors):
         device = t.get_device()                            # -1 on the host
         if device != current:
             if current is None and device >= 0:
-                current = (_torch or _import_torch()).cuda.current_device()
+                current = _torch.cuda.current_device()
             if device != current:
                 raise ValueError(f"a tensor on {t.device}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
     return _stream(current)

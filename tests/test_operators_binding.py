@@ -65,3 +65,32 @@ def test_weights_and_tables_that_became_something_else(change):
     weight.untyped_storage().resize_(0)                      # as sharded parameters have it between their uses
     with pytest.raises(ValueError, match="without memory"):
         calls(s, norm, None)[0]()
+
+
+# ---- gradients ----------------------------------------------------------------------------------
+def test_gradients_are_not_lost_in_silence():
+    """These calls record nothing: a tensor that autograd waits for is refused, unless the program has said that it does not."""
+    s, x, w = shape(), torch.zeros(1, 2, 30, 128, dtype=BF16), torch.zeros(fps.mx4_bytes(9, 256), dtype=U8)
+    leaf, weight, rows = x.clone().requires_grad_(), torch.ones(128, requires_grad=True), torch.zeros(30, 256, requires_grad=True)
+    norm, out = fps.make_norm(weight), torch.zeros(30, 9)
+    asked = [lambda: fps.norm_rotate(s, leaf), lambda: fps.norm_rotate(s, leaf * 2), lambda: fps.norm_rotate(s, x, norm), lambda: fps.norm_rotate(s, x, out=leaf),
+             lambda: fps.norm_rotate_operand(s, leaf, fps.ROLE_Q), lambda: fps.norm_rotate_operand(s, x, fps.ROLE_Q, norm=norm),
+             lambda: fps.norm_rotate_bwd(s, leaf, x), lambda: fps.norm_rotate_bwd(s, x, leaf), lambda: fps.norm_rotate_bwd(s, x, x, norm),
+             lambda: fps.mx4_quantize(rows), lambda: fps.mx4_linear(rows, w, 9), lambda: fps.mx4_linear(rows.detach(), w, 9, bias=torch.zeros(9, requires_grad=True)),
+             lambda: fps.mx4_dequantize(w, 30, 9, out=rows[:, :9])]
+    for call in asked:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        for quiet in (torch.no_grad, torch.inference_mode):
+            with quiet(), pytest.raises(ValueError, match="current device"):
+                call()
+    with pytest.raises(ValueError, match="current device"):
+        fps.norm_rotate(s, leaf.detach())
+
+    class Own(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, t):
+            return fps.norm_rotate(s, t)
+
+    with pytest.raises(ValueError, match="current device"):
+        Own.apply(leaf)
