@@ -79,14 +79,15 @@ class FpsError(RuntimeError):
 
 _lib = None
 _torch = None                                  # the module, once a device entry point has needed it
+_written = None                                # marks what a call has written into: autograd then takes it no longer for what it saved
 _codes = {}                                    # of torch's types, from then on
 
 
 def _import_torch():
-    global _torch
+    global _torch, _written
     if _torch is None:
         import torch
-        _torch = torch
+        _torch, _written = torch, torch.autograd.graph.increment_version
     return _torch
 
 
@@ -379,21 +380,22 @@ def attn_fwd(shape: Shape, window, prec, q, k, v, sq=None, sk=None, sv=None, vsc
 def _here(*tensors):
     """Every tensor (None: left out) is on the current device and autograd waits for a gradient of none; returns its stream, which the call
     goes to."""
-    if (_torch or _import_torch()).is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("a tensor requires a gradient, which this call does not record: make it under torch.no_grad(), or in an "
-                                 "autograd.Function whose backward calls the gradient's entry point")
-    current = None
+    recording = (_torch or _import_torch()).is_grad_enabled()
+    current = away = None
     for t in tensors:
         if t is None:
             continue
+        if recording and t.requires_grad:
+            raise ValueError("a tensor requires a gradient, which this call does not record: make it under torch.no_grad(), or in an "
+                             "autograd.Function whose backward calls the gradient's entry point")
         device = t.get_device()                            # -1 on the host
         if device != current:
             if current is None and device >= 0:
                 current = _torch.cuda.current_device()
-            if device != current:
-                raise ValueError(f"a tensor on {t.device}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
+            if device != current and away is None:
+                away = t.device
+    if away is not None:
+        raise ValueError(f"a tensor on {away}, not on the current device" + ("" if current is None else f" (cuda:{current})"))
     return _stream(current)
 
 
@@ -512,6 +514,7 @@ def norm_rotate(shape: Shape, x, norm: Norm = None, rotation: Rotation = None, o
                           device=x.device)
     stream = _here(x, out, weight, table)
     _check(lib().fps_norm_rotate(shape, _view(x, "x"), norm, rotation, _view(out, "out"), stream))
+    _written(out)
     return out
 
 
@@ -531,6 +534,7 @@ def norm_rotate_operand(shape: Shape, x, role, prec=PREC_FP8, norm: Norm = None,
     if fp8:
         _whole(scales, torch.float32, shape.B * shape.heads * num_groups(shape), "scales")
     _check(lib().fps_norm_rotate_operand(shape, _view(x, "x"), norm, rotation, role, prec, out.data_ptr(), _ptr(scales), stream))
+    _written((out, scales) if fp8 else out)
     return out, scales
 
 
@@ -562,6 +566,7 @@ def norm_rotate_bwd(shape: Shape, x, dy, norm: Norm = None, rotation: Rotation =
     stream = _here(x, dy, dx, dweight, workspace, weight, table)
     _check(lib().fps_norm_rotate_bwd(shape, _view(x, "x"), norm, rotation, _view(dy, "dy"), _view(dx, "dx"), _ptr(dweight),
                                      _ptr(workspace), size, stream))
+    _written(dx if dweight is None else (dx, dweight))
     return dx, dweight
 
 
@@ -577,6 +582,7 @@ def dequantize(shape: Shape, xq, scales, role, vscale=VSCALE_TILE, out=None, out
     n = shape.head_dim if role == ROLE_V and vscale == VSCALE_CHANNEL else num_groups(shape)
     _whole(scales, torch.float32, shape.B * shape.heads * n, "scales")
     _check(lib().fps_dequantize(shape, xq.data_ptr(), scales.data_ptr(), role, vscale, _dtype_code(out), out.data_ptr(), stream))
+    _written(out)
     return out
 
 
@@ -623,6 +629,7 @@ def mx4_quantize(x, out=None):
     stream = _here(x, out)
     _whole(out, torch.uint8, n, "out")
     _check(lib().fps_mx4_quantize(v, out.data_ptr(), stream))
+    _written(out)
     return out
 
 
@@ -637,6 +644,7 @@ def mx4_dequantize(packed, rows, cols, out=None, out_dtype=None):
         raise ValueError(f"out {tuple(out.shape)} is not a matrix of {rows} x {cols}")
     _whole(packed, torch.uint8, mx4_bytes(rows, cols), "packed")
     _check(lib().fps_mx4_dequantize(packed.data_ptr(), v, stream))
+    _written(out)
     return out
 
 
@@ -660,6 +668,7 @@ def mx4_matmul(a, b, m, n, k, bias=None, out=None, out_dtype=None):
     if bias is not None:
         _whole(bias, torch.float32, n, "bias")
     _check(lib().fps_mx4_matmul(k, a.data_ptr(), b.data_ptr(), _ptr(bias), v, stream))
+    _written(out)
     return out
 
 
@@ -676,4 +685,5 @@ def mx4_linear(x, w, n, bias=None, out=None, out_dtype=None, workspace=None):
     if bias is not None:
         _whole(bias, torch.float32, n, "bias")
     _check(lib().fps_mx4_linear(xv, w.data_ptr(), _ptr(bias), v, workspace.data_ptr(), size, stream))
+    _written(out)
     return out
