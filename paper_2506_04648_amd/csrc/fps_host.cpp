@@ -22,6 +22,12 @@ int hip_fail(hipError_t e, const char* what) {
     return FPS_ERR_HIP;
 }
 
+int check_launch(long long workgroups, int threads, const char* what) {
+    if (workgroups * threads <= 0xFFFFFFFFLL) return FPS_OK;
+    set_error("%s: more than a launch has threads for", what);
+    return FPS_ERR_UNSUPPORTED;
+}
+
 int check_ptr(const void* p, const char* name) {
     if (!p) { set_error("%s is NULL", name); return FPS_ERR_INVALID_ARG; }
     if (reinterpret_cast<uintptr_t>(p) & 15u) {

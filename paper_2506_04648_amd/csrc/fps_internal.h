@@ -178,6 +178,7 @@ int check_shape(const fps_shape* s, Geom* g);          // validates, fills g
 int check_ptr(const void* p, const char* name);        // non-null and 16-byte aligned
 int check_enum(int v, int hi, const char* name);
 int hip_fail(hipError_t e, const char* what);          // records and returns FPS_ERR_HIP
+int check_launch(long long workgroups, int threads, const char* what);      // a launch has less than 2^32 threads
 
 // kernel launchers (defined in the .hip files); all arguments already validated
 int launch_tile_order(const Geom& g, const void* in, void* out, hipStream_t st);

@@ -330,6 +330,7 @@ int launch_mx4_quantize(const fps_view& v, void* packed, hipStream_t st) {
     const Matrix x(v);
     const Packed p(packed, x.all_rows(), x.all_cols());
     const int at = p.tiles * p.steps;
+    FPS_TRY(check_launch((at + 3) / 4, 256, "mx4_quantize"));
     auto launch = [&](auto f32, auto qs) {
         constexpr int QS = decltype(qs)::value;
         const int waves = QS == 4 ? at : 4 * at;
@@ -352,6 +353,7 @@ int launch_mx4_dequantize(const void* packed, const fps_view& v, hipStream_t st)
     const Matrix y(v);
     const Packed p(packed, y.all_rows(), y.all_cols());
     const int waves = p.tiles * p.steps, grid = (waves + 3) / 4;
+    FPS_TRY(check_launch(grid, 256, "mx4_dequantize"));
     if (v.dt == FPS_OUT_F32) mx4_dequantize_kernel<true><<<grid, 256, 0, st>>>(p, y, waves);
     else                     mx4_dequantize_kernel<false><<<grid, 256, 0, st>>>(p, y, waves);
     hipError_t e = hipGetLastError();
@@ -361,7 +363,7 @@ int launch_mx4_dequantize(const void* packed, const fps_view& v, hipStream_t st)
 template <int KW>
 static int launch_direct(const Packed& a, const Packed& b, const float* bias, const fps_view& v, hipStream_t st) {
     const long long grid = (long long)a.tiles * b.tiles;
-    if (grid > 0x7FFFFFFF) { set_error("more tiles than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
+    FPS_TRY(check_launch(grid, 64 * KW, "mx4_matmul"));
     if (v.dt == FPS_OUT_F32) mx4_matmul_kernel<KW, true><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v));
     else                     mx4_matmul_kernel<KW, false><<<(int)grid, 64 * KW, 0, st>>>(a, b, bias, Matrix(v));
     hipError_t e = hipGetLastError();

@@ -659,7 +659,7 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
     const bool few = blocks * x.B * x.heads < 1024;
     const int parts = few ? x.heads : (x.heads + kHeads - 1) / kHeads;
     const long long grid = blocks * x.B * parts;
-    if (grid > 0x7FFFFFFF) { set_error("more rows than a launch has workgroups for"); return FPS_ERR_UNSUPPORTED; }
+    FPS_TRY(check_launch(grid, 256, "norm_rotate"));
     const bool past = beyond_caches(x, y);
     with(x.dt == FPS_OUT_F32, [&](auto in32) { with(y.dt == FPS_OUT_F32, [&](auto out32) { with(halves(rot), [&](auto hv) { with(past, [&](auto pa) {
         auto launch = [&](auto hc) {
@@ -675,8 +675,8 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
 }
 
 template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY, bool PAST, bool OWN>
-static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
-                           hipStream_t st) {
+static int launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
+                          hipStream_t st) {
     // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
     // be more threads than a workgroup may have
     constexpr int TH = BS == 128 ? 512 : 128;
@@ -685,28 +685,34 @@ static void launch_operand(const Geom& g, const Rows& x, const Turning& k, int h
         const int each = many ? kManyHeads : 1, parts = (heads + each - 1) / each;
         return Launch{Units{each, parts, count, reciprocal(count)}, g.BH / heads * parts * count};
     };
+    auto check = [](const Launch& l, int threads) { return check_launch(l.grid, threads, "norm_rotate_operand"); };
     const Launch blocks = of_head(g.M * g.KB, MANY);
     const int groups = g.BH * g.M * g.NS;
     if (prec != FPS_PREC_FP8) {
+        FPS_TRY(check(blocks, TH));
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, false, 1, kWhole, STAGED, MANY, PAST, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
-        return;
+        return FPS_OK;
     }
     auto whole = [&](auto nb) {
         constexpr int NB = decltype(nb)::value, T = TH * NB > 1024 ? TH / 2 : TH;
         constexpr bool many = MANY && T == TH;               // twice the rows a lane: no registers for the next head's
         const Launch l = of_head(g.M * g.NS, many);
+        FPS_TRY(check(l, T * NB));
         norm_rotate_operand_kernel<BS, T, IN32, HALVES, true, NB, kWhole, STAGED, many, many && PAST, many && OWN><<<l.grid, T * NB, 0, st>>>(x, k, xq, scales, role, g, heads, l.units);
+        return (int)FPS_OK;
     };
-    if (g.KBS == 1)      whole(Count<1>{});
-    else if (g.KBS == 2) whole(Count<2>{});
-    else if (g.KBS == 3) whole(Count<3>{});
-    else if constexpr (BS == 128) {                          // blocks of 32 are at most three a group
+    if (g.KBS == 1) return whole(Count<1>{});
+    if (g.KBS == 2) return whole(Count<2>{});
+    if (g.KBS == 3) return whole(Count<3>{});
+    if constexpr (BS == 128) {                               // blocks of 32 are at most three a group
         if (g.KBS == 4) return whole(Count<4>{});            // 512 tokens, 1024 threads: one pass instead of two and three launches less
+        FPS_TRY(check(blocks, TH));
         clear_kernel<<<(groups + 255) / 256, 256, 0, st>>>((uint32_t*)scales, groups);     // x is read twice: by way of the caches
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 0, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         norm_rotate_operand_kernel<BS, TH, IN32, HALVES, true, 1, 1, STAGED, MANY, false, OWN><<<blocks.grid, TH, 0, st>>>(x, k, xq, scales, role, g, heads, blocks.units);
         scales_kernel<<<(groups + 255) / 256, 256, 0, st>>>(scales, groups);
     }
+    return FPS_OK;
 }
 
 int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm* norm, const fps_rotation* rot, int role,
@@ -720,8 +726,9 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
     // heads, 540 blocks of 128, 9.6, 11.1.  With weights of each head, which the staged turns then do not hold, beyond the caches: 720p 239, 215
     // (313, 298); 480p 35.0, 36.4
     const bool own = k.weight_head != 0, many = staged && x.heads > 1 && (!own || past) && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
+    int rc = FPS_OK;
     auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn, auto pa, auto ow) {
-        launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value, decltype(pa)::value, decltype(ow)::value>(
+        rc = launch_operand<decltype(big)::value ? 128 : 32, decltype(in32)::value, decltype(hv)::value, decltype(sg)::value, decltype(mn)::value, decltype(pa)::value, decltype(ow)::value>(
             g, rows_of(x), k, x.heads, role, prec, (uint8_t*)xq, scales, st);
     };
     with(g.BS == 128, [&](auto big) { with(halves(rot), [&](auto hv) {
@@ -732,6 +739,7 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
         else if (many)           with(past, [&](auto pa) { launch(big, no, hv, yes, yes, pa, no); });
         else                     with(staged, [&](auto sg) { launch(big, no, hv, sg, no, no, no); });
     }); });
+    if (rc != FPS_OK) return rc;
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? FPS_OK : hip_fail(e, "norm_rotate_operand launch");
 }
@@ -752,6 +760,7 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
     const bool per_head = norm && norm->per_head && norm->weight;
     const int n = bwd_workgroups(g, x.heads, per_head), grid = n * (per_head ? (x.heads + kOwnHeads - 1) / kOwnHeads : 1);
     if (!dweight) partial = nullptr;
+    else if (per_head) FPS_TRY(check_launch(16LL * x.heads, 1024, "norm_rotate_bwd"));
     with(x.dt == FPS_OUT_F32, [&](auto f32) { with(halves(rot), [&](auto hv) { with(per_head, [&](auto own) { with(beyond_caches(x, dx), [&](auto pa) {
         norm_rotate_bwd_kernel<decltype(f32)::value, decltype(hv)::value, decltype(own)::value ? kOwnHeads : kBwdHeads, decltype(own)::value, decltype(pa)::value>
             <<<grid, 256, 0, st>>>(rows_of(x), rows_of(dy), rows_of(dx), k, partial, x.rows, x.heads, x.B, n);
@@ -764,6 +773,7 @@ int launch_norm_rotate_bwd(const Geom& g, const fps_view& x, const fps_norm* nor
 int launch_dequantize(const Geom& g, const void* xq, const float* scales, int role, bool per_channel, bool f32, void* out,
                       hipStream_t st) {
     const int blocks = g.BH * g.M * g.KB;
+    FPS_TRY(check_launch(blocks, 256, "dequantize"));
     with(g.BS == 128, [&](auto big) { with(f32, [&](auto f) { with(role == FPS_ROLE_V, [&](auto v) {
         dequantize_kernel<decltype(big)::value ? 128 : 32, decltype(f)::value, decltype(v)::value>
             <<<blocks, 256, 0, st>>>((const uint8_t*)xq, scales, role, per_channel, (char*)out, g);

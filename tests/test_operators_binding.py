@@ -94,3 +94,29 @@ def test_gradients_are_not_lost_in_silence():
 
     with pytest.raises(ValueError, match="current device"):
         Own.apply(leaf)
+
+
+# ---- launches -----------------------------------------------------------------------------------
+def test_calls_that_a_launch_has_not_the_threads_for():
+    """2^32 threads and more are refused before anything is launched; the addresses are never followed."""
+    L, at, many = fps.lib(), 0x10000, 1 << 20
+
+    def view(B, heads, rows, cols=128, dt=fps.OUT_BF16):
+        return fps.View(at, dt, B, heads, rows, cols, heads * rows * cols, rows * cols, cols)
+
+    def refused(status):
+        assert status == fps.FPS_ERR_UNSUPPORTED and "threads" in fps.last_error()
+
+    s, v = fps.make_shape(1, (1, 16, 32), (1, 8, 16), B=many), view(many, 1, 512)            # 16 blocks of 32 rows
+    refused(L.fps_norm_rotate(s, v, None, None, v, None))
+    s, v = fps.make_shape(1, (1, 8, 128), (1, 8, 16), B=many), view(many, 1, 1024)           # 8 blocks of 128 slots, 512 threads each
+    refused(L.fps_norm_rotate_operand(s, v, None, None, fps.ROLE_Q, fps.PREC_FP8, at, at, None))
+    s, v = fps.make_shape(1, (1, 4, 8), (1, 1, 1), B=many), view(many, 1, 32)                # 32 blocks of 32 slots, 128 threads each
+    refused(L.fps_norm_rotate_operand(s, v, None, None, fps.ROLE_K, fps.PREC_BF16, at, None, None))
+    refused(L.fps_dequantize(s, at, at, fps.ROLE_Q, fps.VSCALE_TILE, fps.OUT_BF16, at, None))
+    s, v, norm = fps.make_shape(1 << 18, (1, 1, 1), (1, 1, 1)), view(1, 1 << 18, 1), fps.Norm(at, 1, 1e-6)
+    need = L.fps_norm_rotate_bwd_bytes(s, norm)
+    refused(L.fps_norm_rotate_bwd(s, v, norm, None, v, v, at, at, need, None))
+    refused(L.fps_mx4_matmul(1, at, at, None, view(1, 1, 1, 1 << 29), None))
+    refused(L.fps_mx4_quantize(view(1, 1, 1 << 30, 512), at, None))
+    refused(L.fps_mx4_dequantize(at, view(1, 1, 1 << 30, 512), None))
