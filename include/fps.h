@@ -277,7 +277,8 @@ typedef struct {
 } fps_view;
 
 /* Norm over the 128 channels of each token of each head: x -> x * (mean(x^2) + eps)^(-1/2) * weight, in fp32.
- * weight: fp32 (device), [128] or, per_head != 0, [heads,128]; NULL = ones.  eps is a normal float > 0. */
+ * weight: fp32 (device), [128] or, per_head != 0, [heads,128]; NULL = ones.  eps is a normal float > 0.  (Not the norm over a token's whole
+ * row of heads*128 channels that some models take before they split it.) */
 typedef struct { const float* weight; int per_head; float eps; } fps_norm;
 
 typedef enum {
@@ -288,7 +289,7 @@ typedef enum {
 /* Rotation by the token's place: pair p of token (t,h,w), (x,y) -> (x cos - y sin, x sin + y cos).  The first pairs_t pairs
  * turn with t, the next pairs_h with h, the next pairs_w with w; what is left of the 64 stays.  table: fp32 (device), (cos, sin)
  * of [T,pairs_t], then [H,pairs_h], then [W,pairs_w], not looked at if no pair turns; stride_b is the distance in floats between the
- * tables of two batch elements, even and not negative, 0 if they share one.  It is as long as the axes, not as the tokens: 20 KB at
+ * tables of two batch elements, even and not negative, 0 if they share one.  It is as long as the axes, not as the tokens: 24 KB at
  * 720p, which stay in the caches while the tokens pass. */
 typedef struct {
     const float* table;

@@ -370,18 +370,18 @@ static int launch_direct(const Packed& a, const Packed& b, const float* bias, co
     return e == hipSuccess ? FPS_OK : hip_fail(e, "mx4_matmul launch");
 }
 
-// Which product.  us of the product alone, rows x K x columns:
+// Which product.  us of the product alone, captured and replayed, rows x K x columns:
 //   straight into registers (tiles of 32, K shared by 4 / 8 waves) against tiles of 128 by way of LDS, of which there are
-//     1 x 5120 x 30720     13.8 / 13.8    14.9   240       300 x 1536 x 4608     6.1 /  7.6     6.6   108
-//     128 x 5120 x 5120     7.4 /  7.8    11.5    40       64 x 5120 x 15360    12.2 / 13.4    12.8   120
-//     96 x 20480 x 5120    18.3 / 20.0    34.3    40       400 x 1536 x 4608     7.0 /  9.6     6.7   144
-//     256 x 5120 x 5120    10.9 / 11.6    12.1    80       33 x 5120 x 30720    25.5 / 25.1    15.4   240
-//     1 x 20480 x 5120     12.4 / 11.7     -              1024 x 5120 x 5120    35.7 / 38.1    20.8   320
+//     1 x 5120 x 30720     13.4 / 13.3    14.6   240       300 x 1536 x 4608     5.5 /  6.4     6.0   108
+//     128 x 5120 x 5120     6.4 /  6.3    10.9    40       64 x 5120 x 15360    11.6 / 12.7    11.4   120
+//     96 x 20480 x 5120    17.5 / 19.2    33.2    40       400 x 1536 x 4608     6.0 /  7.9     6.1   144
+//     256 x 5120 x 5120     9.6 /  9.5    11.1    80       33 x 5120 x 30720    25.1 / 24.9    15.3   240
+//     1 x 20480 x 5120     11.9 / 11.3    32.6    40       851 x 1536 x 4608    10.8 / 14.1     7.0   252
 //   so those of 128 from 112 of them on, with more rows than 32; eight waves only for few tiles and a long K;
 //   tiles of 256, one a CU at a time, against tiles of 128, two a CU that take 1.7 of the time together (3.4 for 5 where there are many):
-//     2048 x 5120 x 5120    36.9   32.4                     32760 x 1536 x 1536  46.9   48.5
-//     4255 x 1536 x 4608    29.3   22.2                     8192 x 5120 x 5120    108    116
-//     8000 x 1536 x 1536    18.4   17.2                     75600 x 5120 x 5120   965   1088
+//     2048 x 5120 x 5120    33.8   34.3                     32760 x 1536 x 1536  54.5   52.3
+//     4255 x 1536 x 4608    28.7   24.0                     8192 x 5120 x 5120    110    113
+//     8000 x 1536 x 1536    18.0   16.6                     75600 x 5120 x 5120   887   1116
 //   which the rounds of 256 tiles that the CUs make tell apart.
 int launch_mx4_matmul(int K, const void* a, const void* b, const float* bias, const fps_view& v, hipStream_t st) {
     const Packed pa(a, (long long)v.B * v.rows, K), pb(b, (long long)v.heads * v.cols, K);

@@ -5,9 +5,11 @@
 // is a slot of a ring of four in the LDS; a slot is filled again as soon as it is read, three of them before it is needed, across the
 // end of a tile as well.  Of results with fewer tiles, 128 x 128 elements in the same manner, two workgroups a CU.
 //
-// Bound by the matrix instructions and by the power they take: alone they reach 6.0 to 6.8 PFLOP/s (10 at the nominal clock).  75600 x 5120 x 5120
-// 887 us, 4.5 PFLOP/s; 16384 x 16384 x 16384 1.77 ms, 5.0.  (A whole step copied ahead instead of the
-// ring, 16384^3 1.93 ms; the result stored between the tiles instead of among the next one's multiplications, 32760 x 1536 x 4608 166 us instead of 143.)
+// 75600 x 5120 x 5120 887 us, 4.5 PFLOP/s; 16384 x 16384 x 16384 1.80 ms, 4.9.  The matrix unit is busy in 62 % (71 %) of the cycles, at the 1.5 to
+// 1.6 GHz that the chip's power leaves it (at 2.4 GHz its peak is 10 PFLOP/s); in the others its wave waits.  Of memory
+// 0.90 GB (1.72) are read, 4 (6) times the operands.  (A whole step copied ahead instead of the
+// ring, 16384^3 1.93 ms; the result stored between the tiles instead of among the next one's multiplications, 32760 x 1536 x 4608 166 us instead of 143.
+// So are results in fp32, or in rows that are not multiples of 8 elements: 75600 x 5120 x 5120 1042 and 955 us, 32760 x 1536 x 4608 221 and 165.)
 #include "fps_mx4.h"
 
 namespace fps {
@@ -386,8 +388,9 @@ static int launch_tiles(const void* pa, const void* pb, int K, const float* bias
         // batch whose elements do not follow each other is written between the tiles
         const bool chunks = y.all_cols() % 8 == 0 && (y.stride_h | y.stride_r) % 16 == 0;
         const bool near = y.stride_r < (1 << 22) && 128 * y.stride_r + (y.heads - 1) * y.stride_h + 2LL * y.cols < 0xFFFFFFF0LL;
-        // and past the caches, which keep the operands, where the result is more than the Infinity Cache's 256 MB: 75600 x 5120 x 5120 909 -> 887 us,
-        // 32760 x 1536 x 4608 148 -> 140; of less, which the cache holds for what reads it next, 8192 x 5120 x 5120 117, 116
+        // and past the caches, which keep the operands, where the result is more than the Infinity Cache's 256 MB: 75600 x 5120 x 5120 897 -> 887 us,
+        // with its quantisation 1061 -> 1037, 32760 x 1536 x 4608 143 -> 138 (173 -> 157); of less, which the cache holds for what reads it next, 8192 x
+        // 5120 x 5120 111, 112
         const bool past = 2LL * y.all_rows() * y.all_cols() > (256LL << 20);
         if (v.dt == FPS_OUT_F32)               mx4_large_kernel<4, true, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);
         else if (y.B > 1 || !chunks || !near)  mx4_large_kernel<4, false, false, false><<<map.workgroups, 256, 0, st>>>(a, b, bias, y, map);

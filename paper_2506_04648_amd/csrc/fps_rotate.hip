@@ -6,7 +6,7 @@
 //
 // All of it is bound by HBM: some ten operations an element.  Eight lanes hold a row of 128 channels, 16 channels or 8
 // pairs each, so that a row is two (four) 16-byte loads of each lane, the sum over it three exchanges between neighbouring
-// lanes, and a pair never leaves its lane.  The rotation's tables are as long as the axes: 20 KB at 720p, read from the caches.
+// lanes, and a pair never leaves its lane.  The rotation's tables are as long as the axes: 24 KB at 720p, read from the caches.
 #include "fps_device_common.h"
 
 namespace fps {
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(THREADS * NB) void norm_rotate_operand_kernel(Rows 
         float m = 0.0f;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            // a wave's rows of padding alone: tile (4,16,16), half of it outside the grid, 190 -> 172 us, BF16 of 480p 44.4 -> 41.3
+            // a wave's rows of padding alone: tile (4,16,16) of 480p 70.7 -> 62.8 us, of 10 x 40 x 40 tokens of 20 heads 65.7 -> 62.4, BF16 of 480p 40.1 -> 38.8
             if (org.slot0 + kb * BS + (__builtin_amdgcn_readfirstlane(tid >> 6) << 3) + THREADS / 8 * i >= org.box.n) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[i].a[j] = y[i].b[j] = 0.0f;
@@ -643,7 +643,8 @@ static bool halves(const fps_rotation* rot) { return rot && rot->pairing == FPS_
 // Heads a workgroup takes together.  us: forward, 720p of 40 heads, 480p of 12, 720p of 3: 2 292, 32.3, 20.3; 4 281, 31.4, 20.3; 8 286, 31.8,
 // 22.3; 16 294, 34.6, 24.7.  The gradient with one weight for all, with its second kernel: 2 519, 68, 40; 4 468, 58, 36; 8 476, 67, 36; with
 // weights of each head: 1 508, 70, 40; 2 469, 79, 51; 4 574, 119, 80.  Its workgroups, which stay: 512 468, 58.2, 36.7; 1024 468, 60.5, 35.4;
-// 2048 467, 65, 38; with weights of each head 2048 552, 72, 37; 4096 508, 70, 40; 8192 489, 74, 46.
+// 2048 467, 65, 38; with weights of each head 2048 552, 72, 37; 4096 508, 70, 40; 8192 489, 74, 46.  Weights of each head: one
+// head a workgroup at every size, where two gain 8 % at 720p and lose 13 and 28 % at the others.
 constexpr int kHeads = 4, kBwdHeads = 4, kBwdWorkgroups = 512, kOwnHeads = 1, kOwnWorkgroups = 4096;
 
 // f(bool constants...) for run-time truth values
@@ -677,8 +678,8 @@ int launch_norm_rotate(const Geom& g, const fps_view& x, const fps_norm* norm, c
 template <int BS, bool IN32, bool HALVES, bool STAGED, bool MANY, bool PAST, bool OWN>
 static int launch_operand(const Geom& g, const Rows& x, const Turning& k, int heads, int role, int prec, uint8_t* xq, float* scales,
                           hipStream_t st) {
-    // two rows of a block a lane: with four a wave takes 116 registers and a SIMD holds four of them (720p 280 us); three blocks of 128 would
-    // be more threads than a workgroup may have
+    // two rows of a block a lane: with four 480p 37.7 us instead of 34.7, 720p 228 instead of 222, weights of each head 241 instead of 226; three
+    // blocks of 128 would be more threads than a workgroup may have
     constexpr int TH = BS == 128 ? 512 : 128;
     struct Launch { Units units; int grid; };
     auto of_head = [&](int count, bool many) {
@@ -719,12 +720,12 @@ int launch_norm_rotate_operand(const Geom& g, const fps_view& x, const fps_norm*
                                int prec, void* xq, float* scales, hipStream_t st) {
     const Turning k = turning_of(g, norm, rot);
     const bool staged = (long long)g.Qt * k.ct + (long long)g.Qh * k.ch + (long long)g.Qw * (64 - k.ct - k.ch) <= kStaged;
-    // past the caches: 720p of 40 heads 228 -> 210 us (BF16 306 -> 296); 480p of 12, which they hold, 33.4, 36.3
+    // past the caches: 720p of 40 heads 231 -> 222 us (BF16 307 -> 300); 480p of 12, which they hold, 34.6, 37.7
     const bool past = (long long)x.B * x.heads * x.rows * kHeadDim * (prec == FPS_PREC_FP8 ? 3 : 4) > kCaches;
     // Several heads a workgroup where there are 1024 blocks of 128 slots or more (bf16; fp32 rows leave no registers).  us with one head,
-    // with four: 480p of 12 heads 38.9, 32.7 (BF16 48.8, 43.8), 720p of 40 heads 247, 227 (334, 310), of 3 heads 21.5, 19.5; 4255 tokens of 12
-    // heads, 540 blocks of 128, 9.6, 11.1.  With weights of each head, which the staged turns then do not hold, beyond the caches: 720p 239, 215
-    // (313, 298); 480p 35.0, 36.4
+    // with four: 480p of 12 heads 34.5, 34.7 (BF16 40.6, 38.8), in tiles (4,16,16) 67, 63, 720p of 40 heads 247, 222 (306, 300), of 3 heads 21.9,
+    // 21.9; 4255 tokens of 12 heads, 540 blocks of 128, 9.6, 12.3.  With weights of each head, which the staged turns then do not hold, beyond the
+    // caches: 720p 248, 226 (306, 300); 480p 34.8, 38.7
     const bool own = k.weight_head != 0, many = staged && x.heads > 1 && (!own || past) && (long long)g.BH * g.M * g.KB * g.BS >= 128 * 1024;
     int rc = FPS_OK;
     auto launch = [&](auto big, auto in32, auto hv, auto sg, auto mn, auto pa, auto ow) {
