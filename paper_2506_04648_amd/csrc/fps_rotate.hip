@@ -471,7 +471,8 @@ __global__ __launch_bounds__(256) void norm_rotate_bwd_kernel(Rows x, Rows dy, R
             const Pairs xv = unpack<F32, HALVES>(cx[i]), g0 = unpack<F32, HALVES>(cy[i]);
             Pairs& sum = dw[OWN ? i : 0];
             const float r = inverse_rms(k, xv);
-            const Pairs nv = times(xv, r);                   // at most the row's length: no product below passes fp32's range by x
+            Pairs nv = times(xv, r);                         // at most the row's length: no product below passes fp32's range by x
+            if (!k.norm) nv.a = nv.b = 0.0f;                 // R^T dy alone, whatever x holds
             Pairs g;
             float dot = 0.0f;
 #pragma unroll

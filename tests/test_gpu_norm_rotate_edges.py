@@ -170,6 +170,18 @@ def test_exact_sums_of_the_weights_gradient(case):
     assert torch.equal(dw.double(), want)
 
 
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("halves", [False, True])
+def test_the_gradient_of_a_rotation_alone_does_not_see_x(dt, halves):
+    say("rotation alone", dt, halves)
+    c = Case(grid=(9, 18, 33), heads=9, dt=dt, norm=False, weight="none", halves=halves)
+    dy = torch.randn(c.x.shape, generator=c.gen, device=DEV).to(dt)
+    want, none = fps.norm_rotate_bwd(c.shape, c.x, dy, None, c.rotation)
+    c.x[0, 3, 17, 5], c.x[0, 4, 18], c.x[0, 8, -1, 127] = float("inf"), float("nan"), float("-inf")
+    dx, _ = fps.norm_rotate_bwd(c.shape, c.x, dy, None, c.rotation)
+    assert none is None and torch.equal(dx, want) and bool(dx.isfinite().all())
+
+
 # ---- tensors that are kept from call to call ----------------------------------------------------
 def test_weights_and_tables_that_were_given_other_memory():
     say("other memory")
